@@ -34,6 +34,10 @@
  *     share it and must run one after another (one stream, or ordered streams).
  *   - The library never falls back to the CPU: without a usable GPU every compute entry point
  *     returns WPK_E_HIP.
+ *   - The sequence layers at the end of this file (wpk_linear_*, wpk_causal_conv1d_*, wpk_ssm_*) keep no
+ *     scratch, take no lock and never allocate: what room a call needs is the caller's `workspace`, so calls
+ *     on different streams may overlap wherever their tensors and workspaces differ, and any call may be
+ *     recorded by a stream capture.  Their conventions stand with them.
  */
 #ifndef WPK_H
 #define WPK_H
@@ -49,7 +53,7 @@ enum {
     WPK_OK            = 0,
     WPK_E_BAD_DESC    = -1, /* non-positive size/stride/dilation, negative pad, P<=0 or Q<=0      */
     WPK_E_NULL_PTR    = -2, /* a required pointer argument is NULL                                */
-    WPK_E_UNSUPPORTED = -3, /* dtype other than fp32, layout value out of range, or a tensor beyond 2^30 elements */
+    WPK_E_UNSUPPORTED = -3, /* dtype an operator does not take, layout value out of range, or a size beyond its limits */
     WPK_E_HIP         = -4, /* a HIP runtime call failed; wpk_last_hip_error() has the code       */
     WPK_E_NO_CONFIG   = -5, /* config id out of range, or not legal for this descriptor           */
     WPK_E_BAD_ARG     = -6, /* any other invalid argument (index out of range, bad sizes ...)     */
@@ -58,7 +62,8 @@ enum {
     WPK_E_TOO_LARGE   = -9  /* wpk_conv2d_fwd_noalloc: the layer's packed weights exceed the static scratch */
 };
 
-enum { WPK_F32 = 0 };
+/* Element types.  Convolutions take WPK_F32 alone; the sequence layers take all three. */
+enum { WPK_F32 = 0, WPK_BF16 = 1, WPK_F16 = 2 };
 /* Activation layouts.  Bit 0: x is channels-last [N][H][W][C]; bit 1: y (and a fused residual) is
  * channels-last [N][P][Q][K].  Weights are always [K][C][R][S].  The two mixed values make the
  * kernel that computes a layer also transform the layout (Section 2.1, data layout transformation)
@@ -425,6 +430,102 @@ int wpk_measure_peaks(double sustain_ms, double *mfma_tflops_burst, double *mfma
                       double *copy_gbs, void *stream);
 /* Library version string. */
 const char *wpk_version(void);
+
+/* ---- sequence layers: matrix product, short causal convolution, selective state space scan -------- */
+/*
+ * The operators of a state space mixer layer as a language model serves it: a product that leaves one row
+ * [z | x | B | C | dt] per token, a short causal convolution over the x, B and C part, the scan, and a product
+ * back to the residual stream.  Inference only, like the convolutions.
+ *
+ * Tensors are DEVICE pointers owned by the caller, of the descriptor's dtype unless a type is given, aligned to
+ * their element.  Rows are one per token, dense within, `*_stride` elements apart, so a tensor may be a slice of
+ * longer rows (16-byte aligned rows are read faster).  Outputs may not overlap inputs except where stated.
+ * All sums and states are held in 32 bits; values are rounded once, when stored.
+ *
+ * Requests ("sequences").  The tokens of all requests stand one after another.  `starts` is NULL (every request has
+ * max_length tokens) or sequences + 1 ascending int32 ON THE DEVICE: request i has the rows starts[i] .. starts[i+1]-1,
+ * possibly none.  Values outside 0 .. tokens are clamped to it.  max_length shapes the launch; a request longer than
+ * it is still computed in full.  Rows of no request are left alone.
+ *
+ * States.  A pool has `slots` entries; request i has entry slot_map[i] (int32 on the device; NULL: entry i).  An entry
+ * outside 0 .. slots-1 means that the request starts from zero and leaves no state.  Entries of different requests have
+ * to differ.  A request continues from state_in if that is given and resume (int32 on the device; NULL: all ones) is not
+ * zero for it; it starts from zero otherwise.  What it leaves goes to state_out if that is given; a request of no tokens
+ * leaves what it started from.  state_out may be state_in (the usual case) or a pool apart from it.
+ */
+enum { WPK_ACT_NONE = 0, WPK_ACT_RELU = 1, WPK_ACT_SILU = 2, WPK_ACT_GELU = 3 /* with erf */ };
+
+/* y[i][j] = act(sum_k x[i][k] * w[j][k] + bias[j]) + residual[i][j]
+ * The residual is added behind the activation, where a residual stream passes a layer (the fused convolutions add it
+ * before, where residual blocks of convolutional networks do). */
+typedef struct wpk_linear_desc {
+    int32_t m, n, k;                /* rows of x and y (0 is allowed), columns of y, reduction         */
+    int32_t dtype;                  /* of x, w, bias and residual                                       */
+    int32_t y_dtype;                /* dtype or WPK_F32                                                 */
+    int32_t act;                    /* WPK_ACT_*                                                        */
+    int64_t x_stride, w_stride;     /* elements between rows, >= k, below 2^20                          */
+    int64_t y_stride, residual_stride;   /* >= n                                                        */
+} wpk_linear_desc;
+
+/* Bytes of workspace that wpk_linear_fwd needs for this descriptor (0: none), or a negative status.  Host only. */
+int64_t wpk_linear_workspace_bytes(const wpk_linear_desc *d);
+
+/* x [m][k], w [n][k], bias [n] or NULL, residual [m][n] or NULL (may be y itself, with the same stride and type).
+ * workspace: NULL if none is needed, 16-byte aligned; its contents before and after mean nothing. */
+int wpk_linear_fwd(const wpk_linear_desc *d, const void *x, const void *w, const void *bias, const void *residual,
+                   void *y, void *workspace, void *stream);
+
+/* y[t][c] = act(bias[c] + sum_j w[c][j] * x[t - (width-1) + j][c]), rows before a request's first taken from its state
+ * (zeros without one).  A state is the last width-1 rows of x: [slots][width-1][channels] of the dtype. */
+typedef struct wpk_causal_conv_desc {
+    int32_t sequences, tokens;      /* requests, rows of x and y (0 is allowed for both)                */
+    int32_t max_length;             /* tokens of the longest request, >= 1                              */
+    int32_t channels, width;        /* width 2 .. 8                                                     */
+    int32_t slots;                  /* entries of the state pool (0 without one)                        */
+    int32_t dtype;
+    int32_t act;                    /* WPK_ACT_NONE or WPK_ACT_SILU                                     */
+    int64_t x_stride, y_stride;     /* elements between rows, >= channels                               */
+} wpk_causal_conv_desc;
+
+/* w [channels][width], bias [channels] or NULL */
+int wpk_causal_conv1d_fwd(const wpk_causal_conv_desc *d, const void *x, const void *w, const void *bias,
+                          const int32_t *starts, const int32_t *slot_map, const int32_t *resume, const void *state_in,
+                          void *state_out, void *y, void *stream);
+
+/* One token of every request (tokens == sequences, max_length == 1): row i of x is request i's.  Every request continues. */
+int wpk_causal_conv1d_step(const wpk_causal_conv_desc *d, const void *x, const void *w, const void *bias,
+                           const int32_t *slot_map, const void *state_in, void *state_out, void *y, void *stream);
+
+/* For every head, with its group's B and C (head h has group h / (heads / groups)):
+ *   delta = dt[t][h] + dt_bias[h], through softplus if asked for
+ *   state = exp(delta * a[h]) * state + delta * x[t][h] (outer) B[t]         head_dim x state_dim
+ *   y[t][h] = (state C[t] + d[h] * x[t][h]) * silu(z[t][h])                  terms without their tensor left out
+ * States are fp32 whatever the dtype: [slots][heads][head_dim][state_dim]. */
+typedef struct wpk_ssm_desc {
+    int32_t sequences, tokens;      /* requests, rows (0 is allowed for both)                           */
+    int32_t max_length;             /* tokens of the longest request, >= 1                              */
+    int32_t heads, head_dim;        /* rows of x, z and y are [heads][head_dim]; head_dim <= 256         */
+    int32_t groups, state_dim;      /* rows of B and C are [groups][state_dim]; state_dim <= 256; heads % groups == 0 */
+    int32_t slots;                  /* entries of the state pool (0 without one)                        */
+    int32_t dtype;                  /* of x, dt, b, c, z and y                                          */
+    int32_t dt_softplus;            /* 0 or 1                                                           */
+    int64_t x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride;   /* elements between rows, below 2^22 */
+} wpk_ssm_desc;
+
+/* Bytes of workspace that wpk_ssm_scan_fwd needs for this descriptor (0: none), or a negative status.  Host only. */
+int64_t wpk_ssm_workspace_bytes(const wpk_ssm_desc *d);
+
+/* a [heads], d_skip [heads] or NULL, dt_bias [heads] or NULL: fp32.  z NULL: no gate.  a is as it multiplies delta, below
+ * zero in a layer that forgets.  workspace as for wpk_linear_fwd. */
+int wpk_ssm_scan_fwd(const wpk_ssm_desc *d, const void *x, const void *dt, const float *a, const void *b, const void *c,
+                     const float *d_skip, const void *z, const float *dt_bias, const int32_t *starts,
+                     const int32_t *slot_map, const int32_t *resume, const float *state_in, float *state_out, void *y,
+                     void *workspace, void *stream);
+
+/* One token of every request (tokens == sequences, max_length == 1): row i is request i's.  Every request continues. */
+int wpk_ssm_scan_step(const wpk_ssm_desc *d, const void *x, const void *dt, const float *a, const void *b, const void *c,
+                      const float *d_skip, const void *z, const float *dt_bias, const int32_t *slot_map,
+                      const float *state_in, float *state_out, void *y, void *stream);
 
 #ifdef __cplusplus
 }

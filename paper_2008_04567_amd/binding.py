@@ -13,6 +13,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("WPK_LIBRARY") or os.path.join(_HERE, "libwpk.so")
 N_GENES = 10
 NCHW, X_NHWC, Y_NHWC, NHWC = 0, 1, 2, 3   # layout codes of ConvDesc.layout
+F32, BF16, F16 = 0, 1, 2                  # element types
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 
 (OK, E_BAD_DESC, E_NULL_PTR, E_UNSUPPORTED, E_HIP, E_NO_CONFIG, E_BAD_ARG, E_IO, E_VERIFY,
  E_TOO_LARGE) = (0, -1, -2, -3, -4, -5, -6, -7, -8, -9)
@@ -65,6 +67,24 @@ class TuneReport(ctypes.Structure):
     @property
     def stage_name(self):
         return self.STAGE_NAMES[self.stage] if 0 <= self.stage < 4 else "?"
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("m", "n", "k", "dtype", "y_dtype", "act")] +
+                [(f, ctypes.c_int64) for f in ("x_stride", "w_stride", "y_stride", "residual_stride")])
+
+
+class CausalConvDesc(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("sequences", "tokens", "max_length", "channels", "width", "slots",
+                                               "dtype", "act")] +
+                [(f, ctypes.c_int64) for f in ("x_stride", "y_stride")])
+
+
+class SsmDesc(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("sequences", "tokens", "max_length", "heads", "head_dim", "groups",
+                                               "state_dim", "slots", "dtype", "dt_softplus")] +
+                [(f, ctypes.c_int64) for f in ("x_stride", "dt_stride", "b_stride", "c_stride", "z_stride",
+                                               "y_stride")])
 
 
 GA_CONSTRAINT_FN = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.POINTER(ctypes.c_int32), ctypes.c_int32,
@@ -156,6 +176,13 @@ def lib():
             "wpk_set_workspace_limit": (I, [ctypes.c_int64]),
             "wpk_config_workspace_bytes": (ctypes.c_int64, [P(ConvDesc), P(ConvConfig), ctypes.c_int32,
                                                             P(ctypes.c_int64), P(ctypes.c_int64)]),
+            "wpk_linear_workspace_bytes": (ctypes.c_int64, [P(LinearDesc)]),
+            "wpk_linear_fwd": (I, [P(LinearDesc)] + [V] * 7),
+            "wpk_causal_conv1d_fwd": (I, [P(CausalConvDesc)] + [V] * 10),
+            "wpk_causal_conv1d_step": (I, [P(CausalConvDesc)] + [V] * 8),
+            "wpk_ssm_workspace_bytes": (ctypes.c_int64, [P(SsmDesc)]),
+            "wpk_ssm_scan_fwd": (I, [P(SsmDesc)] + [V] * 16),
+            "wpk_ssm_scan_step": (I, [P(SsmDesc)] + [V] * 13),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -549,3 +576,78 @@ def device_info():
     cus = ctypes.c_int32()
     _check(lib().wpk_device_info(buf, 256, ctypes.byref(cus)), "wpk_device_info")
     return buf.value.decode(), cus.value
+
+
+# ---- sequence layers ------------------------------------------------------------------------------
+def make_linear_desc(m, n, k, dtype=BF16, y_dtype=None, act=ACT_NONE, x_stride=None, w_stride=None, y_stride=None,
+                     residual_stride=None):
+    """LinearDesc; strides are elements between rows and default to dense ones, y_dtype to dtype."""
+    pick = lambda v, default: int(default if v is None else v)
+    return LinearDesc(m, n, k, dtype, pick(y_dtype, dtype), act, pick(x_stride, k), pick(w_stride, k),
+                      pick(y_stride, n), pick(residual_stride, n))
+
+
+def linear_workspace(desc):
+    """Bytes of workspace that linear_fwd needs for this descriptor."""
+    return _check(lib().wpk_linear_workspace_bytes(ctypes.byref(desc)), "wpk_linear_workspace_bytes")
+
+
+def linear_fwd(desc, x, w, y, bias=None, residual=None, workspace=None, stream=None):
+    """y = act(x w^T + bias) + residual."""
+    _check(lib().wpk_linear_fwd(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(y),
+                                _ptr(workspace), _stream(stream)), "wpk_linear_fwd")
+
+
+def make_causal_conv_desc(sequences, tokens, channels, width, max_length=None, slots=0, dtype=BF16, act=ACT_SILU,
+                          x_stride=None, y_stride=None):
+    """CausalConvDesc; max_length defaults to the requests' common length, tokens / sequences."""
+    pick = lambda v, default: int(default if v is None else v)
+    return CausalConvDesc(sequences, tokens, pick(max_length, max(1, tokens // max(1, sequences))), channels, width,
+                          slots, dtype, act, pick(x_stride, channels), pick(y_stride, channels))
+
+
+def causal_conv1d_fwd(desc, x, w, y, bias=None, starts=None, slot_map=None, resume=None, state_in=None,
+                      state_out=None, stream=None):
+    """Short causal convolution over the requests' tokens, continuing from state_in and leaving state_out."""
+    _check(lib().wpk_causal_conv1d_fwd(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(starts),
+                                       _ptr(slot_map), _ptr(resume), _ptr(state_in), _ptr(state_out), _ptr(y),
+                                       _stream(stream)), "wpk_causal_conv1d_fwd")
+
+
+def causal_conv1d_step(desc, x, w, y, bias=None, slot_map=None, state_in=None, state_out=None, stream=None):
+    """The same for one token of every request."""
+    _check(lib().wpk_causal_conv1d_step(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(slot_map),
+                                        _ptr(state_in), _ptr(state_out), _ptr(y), _stream(stream)),
+           "wpk_causal_conv1d_step")
+
+
+def make_ssm_desc(sequences, tokens, heads, head_dim, groups, state_dim, max_length=None, slots=0, dtype=BF16,
+                  dt_softplus=True, x_stride=None, dt_stride=None, b_stride=None, c_stride=None, z_stride=None,
+                  y_stride=None):
+    """SsmDesc; strides default to dense rows, max_length to the requests' common length, tokens / sequences."""
+    pick = lambda v, default: int(default if v is None else v)
+    hp, gn = heads * head_dim, groups * state_dim
+    return SsmDesc(sequences, tokens, pick(max_length, max(1, tokens // max(1, sequences))), heads, head_dim, groups,
+                   state_dim, slots, dtype, 1 if dt_softplus else 0, pick(x_stride, hp), pick(dt_stride, heads),
+                   pick(b_stride, gn), pick(c_stride, gn), pick(z_stride, hp), pick(y_stride, hp))
+
+
+def ssm_workspace(desc):
+    """Bytes of workspace that ssm_scan_fwd needs for this descriptor."""
+    return _check(lib().wpk_ssm_workspace_bytes(ctypes.byref(desc)), "wpk_ssm_workspace_bytes")
+
+
+def ssm_scan_fwd(desc, x, dt, a, b, c, y, d=None, z=None, dt_bias=None, starts=None, slot_map=None, resume=None,
+                 state_in=None, state_out=None, workspace=None, stream=None):
+    """Selective state space scan over the requests' tokens, continuing from state_in and leaving state_out."""
+    _check(lib().wpk_ssm_scan_fwd(ctypes.byref(desc), _ptr(x), _ptr(dt), _ptr(a), _ptr(b), _ptr(c), _ptr(d), _ptr(z),
+                                  _ptr(dt_bias), _ptr(starts), _ptr(slot_map), _ptr(resume), _ptr(state_in),
+                                  _ptr(state_out), _ptr(y), _ptr(workspace), _stream(stream)), "wpk_ssm_scan_fwd")
+
+
+def ssm_scan_step(desc, x, dt, a, b, c, y, d=None, z=None, dt_bias=None, slot_map=None, state_in=None,
+                  state_out=None, stream=None):
+    """The same for one token of every request."""
+    _check(lib().wpk_ssm_scan_step(ctypes.byref(desc), _ptr(x), _ptr(dt), _ptr(a), _ptr(b), _ptr(c), _ptr(d),
+                                   _ptr(z), _ptr(dt_bias), _ptr(slot_map), _ptr(state_in), _ptr(state_out), _ptr(y),
+                                   _stream(stream)), "wpk_ssm_scan_step")
