@@ -1,65 +1,173 @@
 // Selective state space scan: a state of head_dim x state_dim numbers per head, forgotten by exp(delta a) and fed by
 // delta x (outer) B at every token, read out by C.
-#include "wpk_seq.h"
+#include "wpk_ssm_scan.h"
 
 namespace wpk {
 
 static const int kMaxHeadDim = 256, kMaxStateDim = 256;
 
-template <typename T> struct SsmArgs {
-    const T *x, *dt, *b, *c, *z;
-    const float *a, *d_skip, *dt_bias, *state_in;
-    float *state_out;
-    T *y;
-    Requests rq;
-    int32_t heads, head_dim, groups, state_dim, softplus;
-    int64_t x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride;
-};
-
-// One wave per row of a head's state (head_dim rows of state_dim numbers, up to four a lane), token by token.
-template <typename T> __global__ void __launch_bounds__(256) ssm_rows_kernel(SsmArgs<T> a)
+// ---- single tokens -----------------------------------------------------------------------------------------
+// Bound by the states, read and written once: 8 bytes a state element against 5 operations.  A workgroup takes U rows a
+// lane group of one head: LPR lanes hold a row of state_dim numbers, V = 4 (16 bytes) or 1 a lane and CI times that, so
+// every lane has U loads in flight before it needs the first.
+template <typename T, int V, int CI, int U> __global__ void __launch_bounds__(256) ssm_step_kernel(SsmArgs<T> a, int lpr_log)
 {
-    const int lane = threadIdx.x & 63, p = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y, r = blockIdx.z;
-    if (p >= a.head_dim) return;
+    typedef float vec __attribute__((ext_vector_type(V)));
+    const int head = blockIdx.x, r = blockIdx.y, N = a.state_dim, P = a.head_dim;
+    const int lpr = 1 << lpr_log, rows = 256 >> lpr_log;            // rows that a pass of the workgroup holds
+    const int row = threadIdx.x >> lpr_log, at_n = (threadIdx.x & (lpr - 1)) * V;
     int first, length;
     request_rows(a.rq, r, &first, &length);
     const int slot = request_slot(a.rq, r);
-    const bool resume = a.state_in && slot >= 0 && (!a.rq.resume || a.rq.resume[r] != 0);
-    const size_t at = (((size_t)max(slot, 0) * a.heads + head) * a.head_dim + p) * a.state_dim;
-    const int N = a.state_dim, group = head / (a.heads / a.groups);
-    float h[4];
+    const bool resume = a.state_in && slot >= 0, leave = a.state_out && slot >= 0;
+    const size_t at = ((size_t)max(slot, 0) * a.heads + head) * P * N;
+    vec h[U][CI];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = resume && lane + 64 * i < N ? a.state_in[at + lane + 64 * i] : 0.0f;
-    const float decay_rate = a.a[head], skip = a.d_skip ? a.d_skip[head] : 0.0f;
-    const float bias = a.dt_bias ? a.dt_bias[head] : 0.0f;
-    for (int t = first; t < first + length; ++t) {
-        float delta = (float)a.dt[(int64_t)t * a.dt_stride + head] + bias;
-        if (a.softplus) delta = softplus(delta);
-        const float keep = expf(delta * decay_rate);
-        const float x = (float)a.x[(int64_t)t * a.x_stride + (int64_t)head * a.head_dim + p];
+    for (int u = 0; u < U; ++u) {
+        const int p = (blockIdx.z * U + u) * rows + row;
+#pragma unroll
+        for (int i = 0; i < CI; ++i) {
+            const int n = at_n + i * V * lpr;
+            h[u][i] = vec(0.0f);
+            if (resume && p < P && n < N) h[u][i] = *(const vec *)(a.state_in + at + (size_t)p * N + n);
+        }
+    }
+    const int group = head / (a.heads / a.groups);
+    const T *const bp = a.b + (int64_t)first * a.b_stride + group * N, *const cp = a.c + (int64_t)first * a.c_stride + group * N;
+    float delta = (float)a.dt[(int64_t)first * a.dt_stride + head] + (a.dt_bias ? a.dt_bias[head] : 0.0f);
+    if (a.softplus) delta = softplus(delta);
+    const float keep = expf(delta * a.a[head]);
+    vec b[CI], c[CI];
+#pragma unroll
+    for (int i = 0; i < CI; ++i)
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int n = at_n + i * V * lpr + k;
+            b[i][k] = n < N ? (float)bp[n] : 0.0f;
+            c[i][k] = n < N ? (float)cp[n] : 0.0f;
+        }
+    const int64_t hp = (int64_t)head * P;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int p = (blockIdx.z * U + u) * rows + row;
+        const bool live = p < P;
+        const float x = live ? (float)a.x[(int64_t)first * a.x_stride + hp + p] : 0.0f;
         const float in = delta * x;
         float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int n = lane + 64 * i;
+        for (int i = 0; i < CI; ++i) {
+            const int n = at_n + i * V * lpr;
+            h[u][i] = keep * h[u][i] + in * b[i];
             if (n < N) {
-                h[i] = keep * h[i] + in * (float)a.b[(int64_t)t * a.b_stride + group * N + n];
-                s = fmaf(h[i], (float)a.c[(int64_t)t * a.c_stride + group * N + n], s);
+#pragma unroll
+                for (int k = 0; k < V; ++k) s = fmaf(h[u][i][k], c[i][k], s);
+                if (leave && live) *(vec *)(a.state_out + at + (size_t)p * N + n) = h[u][i];
             }
         }
-#pragma unroll
-        for (int m = 32; m > 0; m >>= 1) s += __shfl_xor(s, m);
-        if (lane == 0) {
-            if (a.d_skip) s += skip * x;
-            if (a.z) s *= silu_as<T>((float)a.z[(int64_t)t * a.z_stride + (int64_t)head * a.head_dim + p]);
-            a.y[(int64_t)t * a.y_stride + (int64_t)head * a.head_dim + p] = (T)s;
+        for (int m = lpr >> 1; m > 0; m >>= 1) s += __shfl_xor(s, m);
+        if (live && at_n == 0) {
+            if (a.d_skip) s += a.d_skip[head] * x;
+            if (a.z) s *= silu_as<T>((float)a.z[(int64_t)first * a.z_stride + hp + p]);
+            a.y[(int64_t)first * a.y_stride + hp + p] = (T)s;
         }
     }
-    if (a.state_out && slot >= 0)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (lane + 64 * i < N) a.state_out[at + lane + 64 * i] = h[i];
 }
+
+template <typename T> static int launch_step(const SsmArgs<T> &a, int sequences, hipStream_t st)
+{
+    const int V = a.vec_state ? 4 : 1;
+    int lpr_log = 0;
+    while (lpr_log < 6 && (V << lpr_log) < a.state_dim) ++lpr_log;
+    const int rows = 256 >> lpr_log;
+    // eight rows a lane keep enough bytes in flight; two where that would leave compute units without work
+    const int64_t wide = (int64_t)a.heads * sequences * ((a.head_dim + 8 * rows - 1) / (8 * rows));
+    const int U = wide >= 4 * kComputeUnits ? 8 : 2;
+    const dim3 grid(a.heads, sequences, (a.head_dim + U * rows - 1) / (U * rows));
+#define WPK_STEP(V, CI)                                                                                                \
+    do {                                                                                                               \
+        if (U == 8) hipLaunchKernelGGL((ssm_step_kernel<T, V, CI, 8>), grid, dim3(256), 0, st, a, lpr_log);            \
+        else hipLaunchKernelGGL((ssm_step_kernel<T, V, CI, 2>), grid, dim3(256), 0, st, a, lpr_log);                   \
+    } while (0)
+    if (V == 4) WPK_STEP(4, 1);
+    else if (a.state_dim <= 64) WPK_STEP(1, 1);
+    else WPK_STEP(1, 4);
+#undef WPK_STEP
+    WPK_HIP(hipGetLastError());
+    return WPK_OK;
+}
+
+// ---- prompts -----------------------------------------------------------------------------------------------
+static int scan_chunk(int dtype, int state_dim)     // tokens of a chunk (what fits LDS)
+{
+    if (dtype == WPK_BF16) return 64;
+    return dtype == WPK_F16 && state_dim <= 128 ? 64 : 32;
+}
+
+struct ScanShape {
+    int n_parts, part_chunks;
+};
+
+// Requests are cut along their tokens where their heads alone would leave compute units idle.  Every part but a
+// request's last is walked through twice, first for the state that it leaves and then for y.
+static ScanShape scan_shape(const wpk_ssm_desc &d)
+{
+    const int q = scan_chunk(d.dtype, d.state_dim);
+    const int64_t chunks = ((int64_t)d.max_length + q - 1) / q;
+    const int64_t groups = (int64_t)d.sequences * d.heads * ((d.head_dim + 63) / 64);
+    const int64_t room = 2 * kComputeUnits;
+    int64_t parts = groups > 0 ? room / groups : 1;
+    if (parts > 16) parts = 16;
+    if (parts > chunks / 4) parts = chunks / 4;
+    if (parts < 2) return {1, (int)chunks};
+    const int64_t each = (chunks + parts - 1) / parts;
+    return {(int)((chunks + each - 1) / each), (int)each};
+}
+
+static size_t scan_part_bytes(const wpk_ssm_desc &d, const ScanShape &s)
+{
+    return (size_t)d.sequences * d.heads * s.n_parts * d.head_dim * d.state_dim * sizeof(float);
+}
+
+template <typename T, int NPAD, int Q> static int launch_scan(const SsmArgs<T> &a, int sequences, hipStream_t st)
+{
+    const unsigned heads = a.heads * ((a.head_dim + 63) / 64);
+    if (a.n_parts > 1) {
+        hipLaunchKernelGGL((ssm_scan_kernel<T, NPAD, Q, false>), dim3(heads, a.n_parts - 1, sequences), dim3(256), 0, st, a);
+        WPK_HIP(hipGetLastError());
+    }
+    hipLaunchKernelGGL((ssm_scan_kernel<T, NPAD, Q, true>), dim3(heads, a.n_parts, sequences), dim3(256), 0, st, a);
+    WPK_HIP(hipGetLastError());
+    return WPK_OK;
+}
+
+template <typename T> struct ScanLaunch;
+template <> struct ScanLaunch<bf16> {
+    static int go(const SsmArgs<bf16> &a, int sequences, hipStream_t st)
+    {
+        if (a.state_dim <= 32) return launch_scan<bf16, 32, 64>(a, sequences, st);
+        if (a.state_dim <= 64) return launch_scan<bf16, 64, 64>(a, sequences, st);
+        if (a.state_dim <= 128) return launch_scan<bf16, 128, 64>(a, sequences, st);
+        return launch_scan<bf16, 256, 64>(a, sequences, st);
+    }
+};
+template <> struct ScanLaunch<f16> {
+    static int go(const SsmArgs<f16> &a, int sequences, hipStream_t st)
+    {
+        if (a.state_dim <= 32) return launch_scan<f16, 32, 64>(a, sequences, st);
+        if (a.state_dim <= 64) return launch_scan<f16, 64, 64>(a, sequences, st);
+        if (a.state_dim <= 128) return launch_scan<f16, 128, 64>(a, sequences, st);
+        return launch_scan<f16, 256, 32>(a, sequences, st);
+    }
+};
+template <> struct ScanLaunch<float> {
+    static int go(const SsmArgs<float> &a, int sequences, hipStream_t st)
+    {
+        if (a.state_dim <= 32) return launch_scan<float, 32, 32>(a, sequences, st);
+        if (a.state_dim <= 64) return launch_scan<float, 64, 32>(a, sequences, st);
+        if (a.state_dim <= 128) return launch_scan<float, 128, 32>(a, sequences, st);
+        return launch_scan<float, 256, 32>(a, sequences, st);
+    }
+};
 
 static int check_ssm(const wpk_ssm_desc *dp)
 {
@@ -80,16 +188,27 @@ static int check_ssm(const wpk_ssm_desc *dp)
 }
 
 template <typename T>
-static int ssm_typed(const wpk_ssm_desc &d, const void *x, const void *dt, const float *a, const void *b, const void *c,
+static int ssm_typed(const wpk_ssm_desc &d, bool step, const void *x, const void *dt, const float *a, const void *b, const void *c,
                      const float *d_skip, const void *z, const float *dt_bias, const Requests &rq, const float *state_in,
-                     float *state_out, void *y, hipStream_t st)
+                     float *state_out, void *y, void *workspace, hipStream_t st)
 {
+    const size_t e = sizeof(T);
+    auto rows_ok = [&](const void *p, int64_t stride, int v) { return stride % v == 0 && aligned_to(p, v * e < 16 ? v * e : 16); };
+    const ScanShape shape = scan_shape(d);
     SsmArgs<T> args = {(const T *)x, (const T *)dt, (const T *)b, (const T *)c, (const T *)z, a, d_skip, dt_bias, state_in,
                        state_out, (T *)y, rq, d.heads, d.head_dim, d.groups, d.state_dim, d.dt_softplus,
-                       d.x_stride, d.dt_stride, d.b_stride, d.c_stride, d.z_stride, d.y_stride};
-    hipLaunchKernelGGL((ssm_rows_kernel<T>), dim3((d.head_dim + 3) / 4, d.heads, d.sequences), dim3(256), 0, st, args);
-    WPK_HIP(hipGetLastError());
-    return WPK_OK;
+                       d.x_stride, d.dt_stride, d.b_stride, d.c_stride, d.z_stride, d.y_stride,
+                       nullptr, nullptr, shape.n_parts, shape.part_chunks,
+                       d.state_dim % 8 == 0 && rows_ok(b, d.b_stride, 8) && rows_ok(c, d.c_stride, 8),
+                       d.head_dim % 4 == 0 && rows_ok(x, d.x_stride, 4), d.head_dim % 4 == 0 && rows_ok(z, d.z_stride, 4),
+                       d.head_dim % 4 == 0 && rows_ok(y, d.y_stride, 4),
+                       d.state_dim % 4 == 0 && aligned_to(state_in, 16) && aligned_to(state_out, 16)};
+    if (step) return launch_step<T>(args, d.sequences, st);
+    if (shape.n_parts > 1) {
+        args.parts = (float *)workspace;
+        args.part_decay = (float *)((char *)workspace + scan_part_bytes(d, shape));
+    }
+    return ScanLaunch<T>::go(args, d.sequences, st);
 }
 
 static int ssm_call(const wpk_ssm_desc *dp, bool step, const void *x, const void *dt, const float *a, const void *b,
@@ -108,11 +227,15 @@ static int ssm_call(const wpk_ssm_desc *dp, bool step, const void *x, const void
     if (!aligned_to(x, e) || !aligned_to(dt, e) || !aligned_to(b, e) || !aligned_to(c, e) || !aligned_to(z, e) ||
         !aligned_to(y, e) || !aligned_to(a, 4) || !aligned_to(d_skip, 4) || !aligned_to(dt_bias, 4))
         return WPK_E_BAD_ARG;
+    if (!step) {
+        if (wpk_ssm_workspace_bytes(dp) > 0 && !workspace) return WPK_E_NULL_PTR;
+        if (!aligned_to(workspace, 16)) return WPK_E_BAD_ARG;
+    }
     const Requests rq = {starts, slot_map, resume, d.tokens, d.max_length, d.slots};
     const hipStream_t st = (hipStream_t)stream;
-    if (d.dtype == WPK_BF16) return ssm_typed<bf16>(d, x, dt, a, b, c, d_skip, z, dt_bias, rq, state_in, state_out, y, st);
-    if (d.dtype == WPK_F16) return ssm_typed<f16>(d, x, dt, a, b, c, d_skip, z, dt_bias, rq, state_in, state_out, y, st);
-    return ssm_typed<float>(d, x, dt, a, b, c, d_skip, z, dt_bias, rq, state_in, state_out, y, st);
+    if (d.dtype == WPK_BF16) return ssm_typed<bf16>(d, step, x, dt, a, b, c, d_skip, z, dt_bias, rq, state_in, state_out, y, workspace, st);
+    if (d.dtype == WPK_F16) return ssm_typed<f16>(d, step, x, dt, a, b, c, d_skip, z, dt_bias, rq, state_in, state_out, y, workspace, st);
+    return ssm_typed<float>(d, step, x, dt, a, b, c, d_skip, z, dt_bias, rq, state_in, state_out, y, workspace, st);
 }
 
 }  // namespace wpk
@@ -122,7 +245,10 @@ extern "C" {
 int64_t wpk_ssm_workspace_bytes(const wpk_ssm_desc *d)
 {
     const int rc = wpk::check_ssm(d);
-    return rc == WPK_OK ? 0 : rc;
+    if (rc != WPK_OK) return rc;
+    const wpk::ScanShape s = wpk::scan_shape(*d);
+    if (s.n_parts < 2) return 0;
+    return (int64_t)(wpk::scan_part_bytes(*d, s) + (size_t)d->sequences * d->heads * s.n_parts * sizeof(float));
 }
 
 int wpk_ssm_scan_fwd(const wpk_ssm_desc *d, const void *x, const void *dt, const float *a, const void *b, const void *c,
