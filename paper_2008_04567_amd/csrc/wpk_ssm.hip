@@ -10,65 +10,73 @@ static const int kMaxHeadDim = 256, kMaxStateDim = 256;
 // Bound by the states, read and written once: 8 bytes a state element against 5 operations.  A workgroup takes U rows a
 // lane group of one head: LPR lanes hold a row of state_dim numbers, V = 4 (16 bytes) or 1 a lane and CI times that, so
 // every lane has U loads in flight before it needs the first.
-template <typename T, int V, int CI, int U> __global__ void __launch_bounds__(256) ssm_step_kernel(SsmArgs<T> a, int lpr_log)
+template <typename T, int V, int CI, int U> __global__ void __launch_bounds__(256, 4) ssm_step_kernel(SsmArgs<T> a, int lpr_log)
 {
     typedef float vec __attribute__((ext_vector_type(V)));
     const int head = blockIdx.x, r = blockIdx.y, N = a.state_dim, P = a.head_dim;
     const int lpr = 1 << lpr_log, rows = 256 >> lpr_log;            // rows that a pass of the workgroup holds
-    const int row = threadIdx.x >> lpr_log, at_n = (threadIdx.x & (lpr - 1)) * V;
+    const int at_n = (threadIdx.x & (lpr - 1)) * V;
+    const int p0 = blockIdx.z * U * rows + (threadIdx.x >> lpr_log);
     int first, length;
     request_rows(a.rq, r, &first, &length);
-    const int slot = request_slot(a.rq, r);
+    const int slot = __builtin_amdgcn_readfirstlane(request_slot(a.rq, r));
     const bool resume = a.state_in && slot >= 0, leave = a.state_out && slot >= 0;
     const size_t at = ((size_t)max(slot, 0) * a.heads + head) * P * N;
+    const float *const in = a.state_in + at;
+    float *const out = a.state_out + at;
     vec h[U][CI];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int p = (blockIdx.z * U + u) * rows + row;
+    for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int i = 0; i < CI; ++i) {
-            const int n = at_n + i * V * lpr;
+            const int p = p0 + u * rows, n = at_n + i * V * lpr;
             h[u][i] = vec(0.0f);
-            if (resume && p < P && n < N) h[u][i] = *(const vec *)(a.state_in + at + (size_t)p * N + n);
+            if (resume && p < P && n < N) h[u][i] = __builtin_nontemporal_load((const vec *)(in + (unsigned)(p * N + n)));
         }
-    }
     const int group = head / (a.heads / a.groups);
     const T *const bp = a.b + (int64_t)first * a.b_stride + group * N, *const cp = a.c + (int64_t)first * a.c_stride + group * N;
+    const T *const xp = a.x + (int64_t)first * a.x_stride + (int64_t)head * P;
+    const T *const zp = a.z + (int64_t)first * a.z_stride + (int64_t)head * P;
+    T *const yp = a.y + (int64_t)first * a.y_stride + (int64_t)head * P;
     float delta = (float)a.dt[(int64_t)first * a.dt_stride + head] + (a.dt_bias ? a.dt_bias[head] : 0.0f);
-    if (a.softplus) delta = softplus(delta);
-    const float keep = expf(delta * a.a[head]);
-    vec b[CI], c[CI];
+    Raw<T, V> b[CI], c[CI];
 #pragma unroll
-    for (int i = 0; i < CI; ++i)
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int n = at_n + i * V * lpr + k;
-            b[i][k] = n < N ? (float)bp[n] : 0.0f;
-            c[i][k] = n < N ? (float)cp[n] : 0.0f;
-        }
-    const int64_t hp = (int64_t)head * P;
+    for (int i = 0; i < CI; ++i) {
+        const int n = at_n + i * V * lpr;
+        b[i].load(bp + n, true, N - n, a.vec_bc);
+        c[i].load(cp + n, true, N - n, a.vec_bc);
+    }
+    T x[U], z[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int p = (blockIdx.z * U + u) * rows + row;
-        const bool live = p < P;
-        const float x = live ? (float)a.x[(int64_t)first * a.x_stride + hp + p] : 0.0f;
-        const float in = delta * x;
+        const int p = min(p0 + u * rows, P - 1);
+        x[u] = xp[p];
+        z[u] = a.z ? zp[p] : (T)0.0f;
+    }
+    if (a.softplus) delta = softplus(delta);
+    const float keep = expf(delta * a.a[head]), skip = a.d_skip ? a.d_skip[head] : 0.0f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int p = p0 + u * rows;
+        const float in_x = delta * (float)x[u];
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < CI; ++i) {
             const int n = at_n + i * V * lpr;
-            h[u][i] = keep * h[u][i] + in * b[i];
             if (n < N) {
 #pragma unroll
-                for (int k = 0; k < V; ++k) s = fmaf(h[u][i][k], c[i][k], s);
-                if (leave && live) *(vec *)(a.state_out + at + (size_t)p * N + n) = h[u][i];
+                for (int k = 0; k < V; ++k) {
+                    h[u][i][k] = keep * h[u][i][k] + in_x * (float)b[i].v[k];
+                    s = fmaf(h[u][i][k], (float)c[i].v[k], s);
+                }
+                if (leave && p < P) __builtin_nontemporal_store(h[u][i], (vec *)(out + (unsigned)(p * N + n)));
             }
         }
         for (int m = lpr >> 1; m > 0; m >>= 1) s += __shfl_xor(s, m);
-        if (live && at_n == 0) {
-            if (a.d_skip) s += a.d_skip[head] * x;
-            if (a.z) s *= silu_as<T>((float)a.z[(int64_t)first * a.z_stride + hp + p]);
-            a.y[(int64_t)first * a.y_stride + hp + p] = (T)s;
+        if (p < P && at_n == 0) {
+            if (a.d_skip) s += skip * (float)x[u];
+            if (a.z) s *= silu_as<T>((float)z[u]);
+            yp[p] = (T)s;
         }
     }
 }
