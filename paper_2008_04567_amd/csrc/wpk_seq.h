@@ -24,6 +24,7 @@ typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -51,6 +52,82 @@ template <typename T> __device__ inline float apply_act(float v, int act)
     if (act == WPK_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678f));
     return v;
 }
+
+// ---- rows through buffer descriptors: what is outside a tensor reads as zero and is not written, without a branch -----
+typedef __amdgpu_buffer_rsrc_t Rows;
+static const uint32_t kOutside = 0x80000000u;    // an offset that no descriptor reaches
+__device__ inline Rows rows_at(const void *base)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00020000);
+}
+
+// V elements of a row, `left` of them there (none if the row is not): at once, or one by one where rows are not aligned
+template <typename T, int V> struct Piece {
+    static const int words = V * (int)sizeof(T) / 4;
+    typedef T vec_t __attribute__((ext_vector_type(V)));
+    vec_t v;
+
+    // (`step`: bytes that are the same for all lanes)
+    template <bool WIDE> __device__ void load(Rows rows, uint32_t offset, uint32_t step, int left)
+    {
+        if constexpr (WIDE) {
+            const uint32_t at = left > 0 ? offset : kOutside;
+            union {
+                uint32_t w[words];
+                vec_t v;
+            } u;
+            if constexpr (words >= 4) {
+#pragma unroll
+                for (int i = 0; i < words; i += 4) {
+                    const u32x4 q = __builtin_amdgcn_raw_buffer_load_b128(rows, at + 4 * i, step, 0);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) u.w[i + j] = q[j];
+                }
+            } else {
+                const u32x2 q = __builtin_amdgcn_raw_buffer_load_b64(rows, at, step, 0);
+                u.w[0] = q[0];
+                u.w[1] = q[1];
+            }
+            v = u.v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const uint32_t at = i < left ? offset + i * (uint32_t)sizeof(T) : kOutside;
+                if constexpr (sizeof(T) == 2) v[i] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rows, at, step, 0));
+                else v[i] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(rows, at, step, 0));
+            }
+        }
+    }
+
+    template <bool WIDE> __device__ void store(Rows rows, uint32_t offset, uint32_t step, int left) const
+    {
+        if constexpr (WIDE) {
+            const uint32_t at = left > 0 ? offset : kOutside;
+            union {
+                uint32_t w[words];
+                vec_t v;
+            } u;
+            u.v = v;
+            if constexpr (words >= 4) {
+#pragma unroll
+                for (int i = 0; i < words; i += 4) {
+                    u32x4 q = {u.w[i], u.w[i + 1], u.w[i + 2], u.w[i + 3]};
+                    __builtin_amdgcn_raw_buffer_store_b128(q, rows, at + 4 * i, step, 0);
+                }
+            } else {
+                u32x2 q = {u.w[0], u.w[1]};
+                __builtin_amdgcn_raw_buffer_store_b64(q, rows, at, step, 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const uint32_t at = i < left ? offset + i * (uint32_t)sizeof(T) : kOutside;
+                if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)v[i]), rows, at, step, 0);
+                else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, (T)v[i]), rows, at, step, 0);
+            }
+        }
+    }
+};
 
 // ---- requests and their states (wpk.h, "sequence layers") ------------------------------------------------
 struct Requests {

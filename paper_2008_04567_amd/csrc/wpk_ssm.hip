@@ -34,17 +34,18 @@ template <typename T, int V, int CI, int U> __global__ void __launch_bounds__(25
             if (resume && p < P && n < N) h[u][i] = __builtin_nontemporal_load((const vec *)(in + (unsigned)(p * N + n)));
         }
     const int group = head / (a.heads / a.groups);
-    const T *const bp = a.b + (int64_t)first * a.b_stride + group * N, *const cp = a.c + (int64_t)first * a.c_stride + group * N;
+    const Rows brows = rows_at(a.b + (int64_t)first * a.b_stride + group * N);
+    const Rows crows = rows_at(a.c + (int64_t)first * a.c_stride + group * N);
     const T *const xp = a.x + (int64_t)first * a.x_stride + (int64_t)head * P;
     const T *const zp = a.z + (int64_t)first * a.z_stride + (int64_t)head * P;
     T *const yp = a.y + (int64_t)first * a.y_stride + (int64_t)head * P;
     float delta = (float)a.dt[(int64_t)first * a.dt_stride + head] + (a.dt_bias ? a.dt_bias[head] : 0.0f);
-    Raw<T, V> b[CI], c[CI];
+    Piece<T, V> b[CI], c[CI];
 #pragma unroll
     for (int i = 0; i < CI; ++i) {
         const int n = at_n + i * V * lpr;
-        b[i].load(bp + n, true, N - n, a.vec_bc);
-        c[i].load(cp + n, true, N - n, a.vec_bc);
+        b[i].template load<V == 4>(brows, n * (uint32_t)sizeof(T), 0, N - n);
+        c[i].template load<V == 4>(crows, n * (uint32_t)sizeof(T), 0, N - n);
     }
     T x[U], z[U];
 #pragma unroll
@@ -81,9 +82,9 @@ template <typename T, int V, int CI, int U> __global__ void __launch_bounds__(25
     }
 }
 
-template <typename T> static int launch_step(const SsmArgs<T> &a, int sequences, hipStream_t st)
+template <typename T> static int launch_step(const SsmArgs<T> &a, bool vec_bc, int sequences, hipStream_t st)
 {
-    const int V = a.vec_state ? 4 : 1;
+    const int V = a.vec_state && vec_bc ? 4 : 1;
     int lpr_log = 0;
     while (lpr_log < 6 && (V << lpr_log) < a.state_dim) ++lpr_log;
     const int rows = 256 >> lpr_log;
@@ -136,16 +137,21 @@ static size_t scan_part_bytes(const wpk_ssm_desc &d, const ScanShape &s)
     return (size_t)d.sequences * d.heads * s.n_parts * d.head_dim * d.state_dim * sizeof(float);
 }
 
-template <typename T, int NPAD, int Q> static int launch_scan(const SsmArgs<T> &a, int sequences, hipStream_t st)
+template <typename T, int NPAD, int Q, bool WIDE> static int launch_scan_rows(const SsmArgs<T> &a, int sequences, hipStream_t st)
 {
     const unsigned heads = a.heads * ((a.head_dim + 63) / 64);
     if (a.n_parts > 1) {
-        hipLaunchKernelGGL((ssm_scan_kernel<T, NPAD, Q, false>), dim3(heads, a.n_parts - 1, sequences), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((ssm_scan_kernel<T, NPAD, Q, false, WIDE>), dim3(heads, a.n_parts - 1, sequences), dim3(256), 0, st, a);
         WPK_HIP(hipGetLastError());
     }
-    hipLaunchKernelGGL((ssm_scan_kernel<T, NPAD, Q, true>), dim3(heads, a.n_parts, sequences), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((ssm_scan_kernel<T, NPAD, Q, true, WIDE>), dim3(heads, a.n_parts, sequences), dim3(256), 0, st, a);
     WPK_HIP(hipGetLastError());
     return WPK_OK;
+}
+
+template <typename T, int NPAD, int Q> static int launch_scan(const SsmArgs<T> &a, int sequences, hipStream_t st)
+{
+    return a.vec_rows ? launch_scan_rows<T, NPAD, Q, true>(a, sequences, st) : launch_scan_rows<T, NPAD, Q, false>(a, sequences, st);
 }
 
 template <typename T> struct ScanLaunch;
@@ -207,11 +213,10 @@ static int ssm_typed(const wpk_ssm_desc &d, bool step, const void *x, const void
                        state_out, (T *)y, rq, d.heads, d.head_dim, d.groups, d.state_dim, d.dt_softplus,
                        d.x_stride, d.dt_stride, d.b_stride, d.c_stride, d.z_stride, d.y_stride,
                        nullptr, nullptr, shape.n_parts, shape.part_chunks,
-                       d.state_dim % 8 == 0 && rows_ok(b, d.b_stride, 8) && rows_ok(c, d.c_stride, 8),
-                       d.head_dim % 4 == 0 && rows_ok(x, d.x_stride, 4), d.head_dim % 4 == 0 && rows_ok(z, d.z_stride, 4),
-                       d.head_dim % 4 == 0 && rows_ok(y, d.y_stride, 4),
+                       d.state_dim % 8 == 0 && d.head_dim % 4 == 0 && rows_ok(b, d.b_stride, 8) && rows_ok(c, d.c_stride, 8) &&
+                           rows_ok(x, d.x_stride, 4) && (!z || rows_ok(z, d.z_stride, 4)) && rows_ok(y, d.y_stride, 4),
                        d.state_dim % 4 == 0 && aligned_to(state_in, 16) && aligned_to(state_out, 16)};
-    if (step) return launch_step<T>(args, d.sequences, st);
+    if (step) return launch_step<T>(args, rows_ok(b, d.b_stride, 4) && rows_ok(c, d.c_stride, 4), d.sequences, st);
     if (shape.n_parts > 1) {
         args.parts = (float *)workspace;
         args.part_decay = (float *)((char *)workspace + scan_part_bytes(d, shape));

@@ -36,7 +36,7 @@ template <typename T> struct SsmArgs {
     float *part_decay;
     int32_t n_parts;          // parts that a request may have
     int32_t part_chunks;      // chunks of a part (the last one takes what is left)
-    int32_t vec_bc, vec_x, vec_z, vec_y, vec_state;   // rows that vector accesses may be used on
+    int32_t vec_rows, vec_state;   // whether rows (of the tensors, of the states) start at multiples of 16 bytes
 };
 
 template <typename T> struct SsmType;
@@ -57,39 +57,28 @@ template <int LIMIT, int PA, int PB> __device__ inline f32x4 mma_parts(const bf1
     return c;
 }
 
-template <int PARTS> __device__ inline void split(float v, bf16 (&out)[PARTS])
+// values as sums of parts, the largest first
+template <typename BF, int PARTS, typename F> __device__ inline void split(F v, BF (&out)[PARTS])
 {
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) {
-        out[i] = (bf16)v;
-        v -= (float)out[i];
+        out[i] = __builtin_convertvector(v, BF);
+        if (i + 1 < PARTS) v -= __builtin_convertvector(out[i], F);
     }
 }
-
-// Offset of the eight elements `chunk` of row `row` in a matrix of NCH such chunks a row.  Chunks are dealt out so that
-// sixteen consecutive rows' same chunk covers all banks, and rows eight apart (transposing writes) half of them.
-template <int NCH> __device__ inline int lds_at(int row, int chunk)
+template <int PARTS> __device__ inline void parts_of(bf16 v, bf16 (&out)[PARTS]) { out[0] = v; }
+template <int PARTS, typename T> __device__ inline void parts_of(T v, bf16 (&out)[PARTS])
 {
-    const int f = NCH >= 16 ? (row ^ (row >> 4)) & 15 : NCH == 8 ? ((row >> 1) ^ (row >> 4)) & 7 : ((row >> 2) ^ (row >> 4)) & 3;
-    return (row * NCH + (chunk ^ f)) * 8;
-}
-
-template <typename T, int V> struct Raw {
-    typedef T vec __attribute__((ext_vector_type(V), aligned(V * sizeof(T) < 16 ? V * sizeof(T) : 16)));
-    vec v;
-    __device__ void load(const T *p, bool row_ok, int left, bool wide)   // left: columns from p on that exist
-    {
-        if (row_ok && wide && left > 0) {
-            v = *(const vec *)p;
-            return;
-        }
+    float f = (float)v;
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = row_ok && i < left ? p[i] : (T)0.0f;
+    for (int i = 0; i < PARTS; ++i) {
+        out[i] = (bf16)f;
+        f -= (float)out[i];
     }
-};
+}
 
 // One part of a request: FULL computes y and the state at its end, otherwise only what its tokens add to a state.
-template <typename T, int NPAD, int Q, bool FULL> struct SsmScan {
+template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
     static const int NP = SsmType<T>::parts;
     static const int YP = NP == 3 ? 3 : 2;           // parts of what is formed on the way to y
     static const int NB = NPAD / 16, QB = Q / 16, QK = Q / 32, NCH = NPAD / 8, QCH = Q / 8;
@@ -98,27 +87,51 @@ template <typename T, int NPAD, int Q, bool FULL> struct SsmScan {
     static const int kBlocks = Q == 64 ? 12 : 4;      // 16 x 16 blocks of M, those of zeros beside the diagonal included
     static const int kPerWave = kBlocks / 4;
     // M takes the place of B's rows where both do not fit a compute unit's LDS
-    static const bool kAlias = NP * Q * NPAD * 6 + NP * 64 * Q * 2 + YP * Q * Q * 2 + 24 * Q > 163000;
+    static const bool kAlias = NP * (2 * Q * (NPAD + 8) + (NPAD + 64) * (Q + 8)) * 2 + YP * Q * (Q + 8) * 2 + 48 * Q > 163000;
 
-    struct Shared {
-        bf16 bt[NP][NPAD * Q];                        // [n][s]
-        bf16 xt[NP][64 * Q];                          // [p][s]
-        bf16 c[FULL ? NP : 1][FULL ? Q * NPAD : 8];   // [t][n]
-        bf16 b[FULL ? NP : 1][FULL ? Q * NPAD : 8];   // [s][n]
-        bf16 m[FULL && !kAlias ? YP : 1][FULL && !kAlias ? Q * Q : 8];   // [t][s]
-        float sh[Q], sl[Q], delta[Q], into[Q], from[Q];   // S in two floats, delta, exp(S_end - S) delta, exp(S)
-        float keep;
-        int odd[2];                                   // a chunk holds infinities or NaN in x
+    // Rows of LDS matrices are eight elements longer than they have to be: the same columns of sixteen rows cover all banks.
+    // (Of fp32's 256 columns only those of B and C are, and the scalars have one place, formed while chunks are staged.)
+    static const bool kTight = NP == 3 && NPAD == 256;
+    static const int kN = NPAD + 8, kS = kTight ? Q : Q + 8, kSc = kTight ? 1 : 2;
+    // M holds columns up to the end of a row's 32 tokens only
+    static const int kM = Q == 64 ? 32 * 40 + 32 * kS : Q * kS;
+    static __device__ int m_row(int t) { return Q == 64 ? (t < 32 ? t * 40 : t * kS - 32 * (kS - 40)) : t * kS; }
+
+    struct alignas(16) Scalars {
+        alignas(16) float sh[Q], sl[Q], delta[Q], into[Q], from[Q];   // S in two floats, delta, exp(S_end - S) delta, exp(S)
+        float keep[4];
+    };
+    struct alignas(16) Shared {
+        alignas(16) bf16 bt[NP][NPAD * kS];                       // [n][s]
+        alignas(16) bf16 xt[NP][64 * kS];                         // [p][s]
+        alignas(16) bf16 c[FULL ? NP : 1][FULL ? Q * kN : 8];     // [t][n]
+        alignas(16) bf16 b[FULL ? NP : 1][FULL ? Q * kN : 8];     // [s][n]
+        alignas(16) bf16 m[FULL && !kAlias ? YP : 1][FULL && !kAlias ? kM : 8];   // [t][s]
+        Scalars sc[kSc];                              // of the even and the odd chunks
     };
 
     static __device__ bf16 *m_at(Shared &sm, int part, int offset)
     {
-        return kAlias ? &sm.b[0][part * Q * Q + offset] : &sm.m[kAlias ? 0 : part][offset];
+        return kAlias ? &sm.b[0][part * kM + offset] : &sm.m[kAlias ? 0 : part][offset];
+    }
+
+    // What a lane moves: four tokens s.. of eight columns of B and C, or of four rows of X.  Lanes of a wave are dealt out
+    // over tokens and columns so that the transposing writes to LDS meet at most two to a bank.
+    static __device__ void b_task(int task, int *s, int *chunk)
+    {
+        const int high = Q == 64 ? 2 : 1;
+        *s = 4 * ((task & 3) | ((task >> 4) & ((1 << high) - 1)) << 2);
+        *chunk = ((task >> 2) & 3) | (task >> (4 + high)) << 2;
+    }
+    static __device__ void x_task(int task, int *s, int *quad)
+    {
+        *s = 4 * (((task >> 2) & 7) | (Q == 64 ? ((task >> 6) & 1) << 3 : 0));
+        *quad = (task & 3) | ((task >> 5) & 1) << 2 | (task >> (Q == 64 ? 7 : 6)) << 3;
     }
 
     static __device__ void run(const SsmArgs<T> &a, Shared &sm)
     {
-        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
+        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g = lane >> 4;
         const int head = blockIdx.x % a.heads, pblock = blockIdx.x / a.heads, part = blockIdx.y, r = blockIdx.z;
         const int P = a.head_dim, N = a.state_dim, group = head / (a.heads / a.groups);
         int first, length;
@@ -189,50 +202,52 @@ template <typename T, int NPAD, int Q, bool FULL> struct SsmScan {
         const int64_t hp = (int64_t)head * P;
         const T *const xp = a.x + (int64_t)first * a.x_stride + hp, *const dtp = a.dt + (int64_t)first * a.dt_stride + head;
 
-        Raw<T, 8> rb[kBPer][4], rc[FULL ? kBPer : 1][4];
-        Raw<T, 4> rx[kXPer][4];
-        float rdt = 0.0f;
+        Piece<T, 8> rb[kBPer][4], rc[FULL ? kBPer : 1][4];
+        Piece<T, 4> rx[kXPer][4];
+        const uint32_t e = sizeof(T);
+        const uint32_t bs = (uint32_t)a.b_stride * e, cs = (uint32_t)a.c_stride * e, xs = (uint32_t)a.x_stride * e;
         auto fetch = [&](int chunk) {
-            const int t0 = chunk * Q;
+            const int t0 = chunk * Q, left = length - t0;       // rows that there are
+            const Rows brows = rows_at(bp + (int64_t)t0 * a.b_stride), crows = rows_at(cp + (int64_t)t0 * a.c_stride);
+            const Rows xrows = rows_at(xp + (int64_t)t0 * a.x_stride);
 #pragma unroll
             for (int i = 0; i < kBPer; ++i) {
-                const int task = tid + 256 * i, n = (task % NCH) * 8, s = (task / NCH) * 4;
-                if (kBTasks % 256 != 0 && task >= kBTasks) break;
+                int s, n;
+                b_task(tid + 256 * i, &s, &n);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int t = t0 + s + j;
-                    rb[i][j].load(bp + (int64_t)t * a.b_stride + n, t < length, N - n, a.vec_bc);
-                    if (FULL) rc[i][j].load(cp + (int64_t)t * a.c_stride + n, t < length, N - n, a.vec_bc);
+                    const int cols = s + j < left ? N - 8 * n : 0;
+                    rb[i][j].template load<WIDE>(brows, s * bs + n * 8 * e, j * bs, cols);
+                    if (FULL) rc[i][j].template load<WIDE>(crows, s * cs + n * 8 * e, j * cs, cols);
                 }
             }
 #pragma unroll
             for (int i = 0; i < kXPer; ++i) {
-                const int task = tid + 256 * i, q = p_base + (task % 16) * 4, s = (task / 16) * 4;
-                if (kXTasks % 256 != 0 && task >= kXTasks) break;
+                int s, q;
+                x_task(tid + 256 * i, &s, &q);
+                q = p_base + 4 * q;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int t = t0 + s + j;
-                    rx[i][j].load(xp + (int64_t)t * a.x_stride + q, t < length, P - q, a.vec_x);
-                }
+                for (int j = 0; j < 4; ++j)
+                    rx[i][j].template load<WIDE>(xrows, s * xs + q * e, j * xs, s + j < left ? P - q : 0);
             }
-            if (tid < Q) rdt = t0 + tid < length ? (float)dtp[(int64_t)(t0 + tid) * a.dt_stride] : 0.0f;
         };
-        auto stage = [&](int chunk) {
+        auto stage = [&]() {
 #pragma unroll
             for (int i = 0; i < kBPer; ++i) {
-                const int task = tid + 256 * i, n = (task % NCH) * 8, s = (task / NCH) * 4;
-                if (kBTasks % 256 != 0 && task >= kBTasks) break;
+                int s, n;
+                b_task(tid + 256 * i, &s, &n);
+                if (kBTasks % 256 != 0 && tid + 256 * i >= kBTasks) continue;
                 bf16 v[4][8][NP];
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) split<NP>((float)rb[i][j].v[k], v[j][k]);
+                    for (int k = 0; k < 8; ++k) parts_of<NP>((T)rb[i][j].v[k], v[j][k]);
 #pragma unroll
                 for (int q = 0; q < NP; ++q) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const bf16x4 w = {v[0][k][q], v[1][k][q], v[2][k][q], v[3][k][q]};
-                        *(bf16x4 *)&sm.bt[q][lds_at<QCH>(n + k, s >> 3) + (s & 7)] = w;
+                        *(bf16x4 *)&sm.bt[q][(8 * n + k) * kS + s] = w;
                     }
                     if (FULL)
 #pragma unroll
@@ -240,7 +255,7 @@ template <typename T, int NPAD, int Q, bool FULL> struct SsmScan {
                             bf16x8 w;
 #pragma unroll
                             for (int k = 0; k < 8; ++k) w[k] = v[j][k][q];
-                            *(bf16x8 *)&sm.b[q][lds_at<NCH>(s + j, n >> 3)] = w;
+                            *(bf16x8 *)&sm.b[q][(s + j) * kN + 8 * n] = w;
                         }
                 }
                 if (FULL)
@@ -250,81 +265,97 @@ template <typename T, int NPAD, int Q, bool FULL> struct SsmScan {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
                             bf16 u[NP];
-                            split<NP>((float)rc[i][j].v[k], u);
+                            parts_of<NP>((T)rc[i][j].v[k], u);
 #pragma unroll
                             for (int q = 0; q < NP; ++q) w[q][k] = u[q];
                         }
 #pragma unroll
-                        for (int q = 0; q < NP; ++q) *(bf16x8 *)&sm.c[q][lds_at<NCH>(s + j, n >> 3)] = w[q];
+                        for (int q = 0; q < NP; ++q) *(bf16x8 *)&sm.c[q][(s + j) * kN + 8 * n] = w[q];
                     }
             }
-            float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < kXPer; ++i) {
-                const int task = tid + 256 * i, q4 = (task % 16) * 4, s = (task / 16) * 4;
-                if (kXTasks % 256 != 0 && task >= kXTasks) break;
+                int s, q4;
+                x_task(tid + 256 * i, &s, &q4);
+                if (kXTasks % 256 != 0 && tid + 256 * i >= kXTasks) continue;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     bf16 v[4][NP];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float f = (float)rx[i][j].v[k];
-                        sum = fmaf(f, 0.0f, sum);
-                        split<NP>(f, v[j]);
-                    }
+                    for (int j = 0; j < 4; ++j) parts_of<NP>((T)rx[i][j].v[k], v[j]);
 #pragma unroll
                     for (int q = 0; q < NP; ++q) {
                         const bf16x4 w = {v[0][q], v[1][q], v[2][q], v[3][q]};
-                        *(bf16x4 *)&sm.xt[q][lds_at<QCH>(q4 + k, s >> 3) + (s & 7)] = w;
+                        *(bf16x4 *)&sm.xt[q][(4 * q4 + k) * kS + s] = w;
                     }
                 }
             }
-            if (FULL && __any(sum != 0.0f) && lane == 0) sm.odd[chunk & 1] = 1;   // (NaN)
-            if (wave == 0) {
-                // lanes are tokens
-                const bool live = lane < Q && chunk * Q + lane < length;
-                float delta = rdt + dt_bias;
-                if (a.softplus) delta = softplus(delta);
-                if (!live) delta = 0.0f;
-                double s = (double)delta * rate * 1.4426950408889634;
-                if (s < -192.0) s = -192.0;
-                if (!live) s = 0.0;
-#pragma unroll
-                for (int m = 1; m < Q; m <<= 1) {
-                    const double o = __shfl_up(s, m);
-                    if (lane >= m) s += o;
-                }
-                const double end = __shfl(s, Q - 1);
-                if (lane < Q) {
-                    sm.sh[lane] = (float)s;
-                    sm.sl[lane] = (float)(s - (double)(float)s);
-                    sm.delta[lane] = delta;
-                    sm.into[lane] = delta * __builtin_amdgcn_exp2f((float)(end - s));
-                    sm.from[lane] = __builtin_amdgcn_exp2f((float)s);
-                }
-                if (lane == 0) sm.keep = __builtin_amdgcn_exp2f((float)end);
-            }
         };
+        // One wave forms a chunk's scalars, its lanes the tokens, while the others are at the chunk before.
+        float rdt = 0.0f;
+        auto fetch_dt = [&](int chunk) {
+            const int t0 = chunk * Q;
+            Piece<T, 1> d;
+            d.template load<false>(rows_at(dtp + (int64_t)t0 * a.dt_stride), lane * (uint32_t)a.dt_stride * e, 0,
+                                   lane < Q && t0 + lane < length ? 1 : 0);
+            rdt = (float)d.v[0];
+        };
+        auto scalars = [&](int chunk) {
+            Scalars &sc = sm.sc[chunk & (kSc - 1)];
+            const bool live = lane < Q && chunk * Q + lane < length;
+            float delta = rdt + dt_bias;
+            if (a.softplus) delta = softplus(delta);
+            if (!live) delta = 0.0f;
+            double s = (double)delta * rate * 1.4426950408889634;
+            if (s < -192.0) s = -192.0;
+            if (!live) s = 0.0;
+#pragma unroll
+            for (int m = 1; m < Q; m <<= 1) {
+                const double o = __shfl_up(s, m);
+                if (lane >= m) s += o;
+            }
+            const double end = __shfl(s, Q - 1);
+            if (lane < Q) {
+                sc.sh[lane] = (float)s;
+                sc.sl[lane] = (float)(s - (double)(float)s);
+                sc.delta[lane] = delta;
+                sc.into[lane] = delta * __builtin_amdgcn_exp2f((float)(end - s));
+                sc.from[lane] = __builtin_amdgcn_exp2f((float)s);
+            }
+            if (lane == 0) sc.keep[0] = __builtin_amdgcn_exp2f((float)end);
+        };
+        const int kScalarWave = 3;
 
-        if (tid < 2) sm.odd[tid] = 0;
         float total = 1.0f;
-        if (c0 < c1) fetch(c0);
-        __syncthreads();
+        if (c0 < c1) {
+            fetch(c0);
+            if (wave == kScalarWave) {
+                fetch_dt(c0);
+                scalars(c0);
+                fetch_dt(c0 + 1);
+            }
+        }
+        const int p4 = p_base + wave * 16 + 4 * g;      // rows of y that this lane stores
+        const bf16x8 zero8 = {0, 0, 0, 0, 0, 0, 0, 0};
         for (int chunk = c0; chunk < c1; ++chunk) {
-            stage(chunk);
+            stage();
+            if (kTight && chunk > c0 && wave == kScalarWave) {
+                scalars(chunk);
+                fetch_dt(chunk + 1);
+            }
             __syncthreads();
             const int t0 = chunk * Q;
-            Raw<T, 4> rz[FULL ? QB : 1];
-            const int p4 = p_base + wave * 16 + 4 * g;      // rows of y that this lane stores
-            if (FULL && a.z)
+            const Scalars &sc = sm.sc[chunk & (kSc - 1)];
+            Piece<T, 4> rz[FULL ? QB : 1];
+            if (FULL && a.z) {
+                const Rows zrows = rows_at(a.z + (int64_t)(first + t0) * a.z_stride + hp);
+                const uint32_t zs = (uint32_t)a.z_stride * e;
 #pragma unroll
-                for (int i = 0; i < QB; ++i) {
-                    const int t = t0 + 16 * i + col;
-                    rz[i].load(a.z + (int64_t)(first + t) * a.z_stride + hp + p4, t < length, P - p4, a.vec_z);
-                }
+                for (int i = 0; i < QB; ++i)
+                    rz[i].template load<WIDE>(zrows, col * zs + p4 * e, 16 * i * zs, t0 + 16 * i + col < length ? P - p4 : 0);
+            }
             if (chunk + 1 < c1) fetch(chunk + 1);
-            if (tid == 0) sm.odd[(chunk + 1) & 1] = 0;
-            const float keep = sm.keep;
+            const float keep = sc.keep[0];
             total *= keep;
 
             f32x4 acc[FULL ? QB : 1];
@@ -336,13 +367,14 @@ template <typename T, int NPAD, int Q, bool FULL> struct SsmScan {
                     const int k = wave + 4 * i, tb = k < 4 ? k >> 1 : 2 + ((k - 4) >> 2), sb = k < 4 ? k & 1 : (k - 4) & 3;
                     gt[i] = f32x4{0, 0, 0, 0};
                     if (sb > tb) continue;
+                    const int at_b = (16 * sb + col) * kN + 8 * g, at_c = (16 * tb + col) * kN + 8 * g;
 #pragma unroll
                     for (int n = 0; n < NPAD / 32; ++n) {
                         bf16x8 fb[NP], fc[NP];
 #pragma unroll
                         for (int q = 0; q < NP; ++q) {
-                            fb[q] = *(const bf16x8 *)&sm.b[q][lds_at<NCH>(16 * sb + col, 4 * n + g)];
-                            fc[q] = *(const bf16x8 *)&sm.c[q][lds_at<NCH>(16 * tb + col, 4 * n + g)];
+                            fb[q] = *(const bf16x8 *)&sm.b[q][at_b + 32 * n];
+                            fc[q] = *(const bf16x8 *)&sm.c[q][at_c + 32 * n];
                         }
                         gt[i] = mma_parts<NP>(fb, fc, gt[i]);
                     }
@@ -352,21 +384,22 @@ template <typename T, int NPAD, int Q, bool FULL> struct SsmScan {
                 for (int i = 0; i < kPerWave; ++i) {
                     const int k = wave + 4 * i, tb = k < 4 ? k >> 1 : 2 + ((k - 4) >> 2), sb = k < 4 ? k & 1 : (k - 4) & 3;
                     const int t = 16 * tb + col, s0 = 16 * sb + 4 * g;
-                    const f32x4 sh = *(const f32x4 *)&sm.sh[s0], sl = *(const f32x4 *)&sm.sl[s0], dl = *(const f32x4 *)&sm.delta[s0];
-                    const float th = sm.sh[t], tl = sm.sl[t];
-                    bf16x4 w[YP];
+                    f32x4 v = {0, 0, 0, 0};
+                    if (sb <= tb) {
+                        const f32x4 sh = *(const f32x4 *)&sc.sh[s0], sl = *(const f32x4 *)&sc.sl[s0];
+                        const f32x4 dl = *(const f32x4 *)&sc.delta[s0];
+                        const float th = sc.sh[t], tl = sc.sl[t];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float v = gt[i][j] * (__builtin_amdgcn_exp2f((th - sh[j]) + (tl - sl[j])) * dl[j]);
-                        if (s0 + j == t) v += skip;
-                        if (s0 + j > t) v = 0.0f;
-                        bf16 u[YP];
-                        split<YP>(v, u);
+                        for (int j = 0; j < 4; ++j)
+                            v[j] = gt[i][j] * (__builtin_amdgcn_exp2f((th - sh[j]) + (tl - sl[j])) * dl[j]);
+                        if (sb == tb)
 #pragma unroll
-                        for (int q = 0; q < YP; ++q) w[q][j] = u[q];
+                            for (int j = 0; j < 4; ++j) v[j] = s0 + j > t ? 0.0f : s0 + j == t ? v[j] + skip : v[j];
                     }
+                    bf16x4 w[YP];
+                    split(v, w);
 #pragma unroll
-                    for (int q = 0; q < YP; ++q) *(bf16x4 *)m_at(sm, q, lds_at<QCH>(t, s0 >> 3) + (s0 & 7)) = w[q];
+                    for (int q = 0; q < YP; ++q) *(bf16x4 *)m_at(sm, q, m_row(t) + s0) = w[q];
                 }
                 // exp(S) C h0: rows p, column t in the lane
 #pragma unroll
@@ -375,87 +408,84 @@ template <typename T, int NPAD, int Q, bool FULL> struct SsmScan {
 #pragma unroll
                     for (int n = 0; n < NPAD / 32; ++n) {
                         bf16x8 fh[YP];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            bf16 u[YP];
-                            split<YP>(h[2 * n + (j >> 2)][j & 3], u);
-#pragma unroll
-                            for (int q = 0; q < YP; ++q) fh[q][j] = u[q];
-                        }
+                        split(__builtin_shufflevector(h[2 * n], h[2 * n + 1], 0, 1, 2, 3, 4, 5, 6, 7), fh);
 #pragma unroll
                         for (int i = 0; i < QB; ++i) {
                             bf16x8 fc[NP];
-                            const int t = 16 * i + col;
 #pragma unroll
                             for (int q = 0; q < NP; ++q) {
-                                const bf16x4 lo = *(const bf16x4 *)&sm.c[q][lds_at<NCH>(t, 4 * n + (g >> 1)) + 4 * (g & 1)];
-                                const bf16x4 hi = *(const bf16x4 *)&sm.c[q][lds_at<NCH>(t, 4 * n + 2 + (g >> 1)) + 4 * (g & 1)];
+                                const bf16 *const at = &sm.c[q][(16 * i + col) * kN + 32 * n + 4 * g];
+                                const bf16x4 lo = *(const bf16x4 *)at, hi = *(const bf16x4 *)(at + 16);
                                 fc[q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                             }
                             acc[i] = mma_parts<YP>(fh, fc, acc[i]);
                         }
                     }
 #pragma unroll
-                    for (int i = 0; i < QB; ++i) acc[i] *= sm.from[16 * i + col];
+                    for (int i = 0; i < QB; ++i) acc[i] *= sc.from[16 * i + col];
+                }
+                if (!kTight && wave == kScalarWave && chunk + 1 < c1) {
+                    scalars(chunk + 1);
+                    fetch_dt(chunk + 2);
                 }
                 __syncthreads();
+            } else if (!kTight && wave == kScalarWave && chunk + 1 < c1) {
+                scalars(chunk + 1);
+                fetch_dt(chunk + 2);
             }
 
             bf16x8 fx[QK][NP];
 #pragma unroll
             for (int k = 0; k < QK; ++k)
 #pragma unroll
-                for (int q = 0; q < NP; ++q) fx[k][q] = *(const bf16x8 *)&sm.xt[q][lds_at<QCH>(wave * 16 + col, 4 * k + g)];
+                for (int q = 0; q < NP; ++q) fx[k][q] = *(const bf16x8 *)&sm.xt[q][(wave * 16 + col) * kS + 32 * k + 8 * g];
 
             if (FULL) {
-                if (!sm.odd[chunk & 1]) {
+                // Infinities or NaN among x may not meet the zeros of M that stand for later tokens: x times zero finds them.
+                f32x4 odd = {0, 0, 0, 0};
 #pragma unroll
-                    for (int i = 0; i < QB; ++i)
+                for (int k = 0; k < QK; ++k) odd = mma(fx[k][0], zero8, odd);
 #pragma unroll
-                        for (int k = 0; k <= i / 2; ++k) {
-                            bf16x8 fm[YP];
+                for (int i = 0; i < QB; ++i) {
+                    f32x4 sum = acc[i];
 #pragma unroll
-                            for (int q = 0; q < YP; ++q)
-                                fm[q] = *(const bf16x8 *)m_at(sm, q, lds_at<QCH>(16 * i + col, 4 * k + g));
-                            acc[i] = mma_parts<YP>(fx[k], fm, acc[i]);
-                        }
-                } else {
-                    // infinities or NaN among the chunk's x may not meet the zeros of M that stand for later tokens
+                    for (int k = 0; k <= i / 2; ++k) {
+                        bf16x8 fm[YP];
 #pragma unroll
-                    for (int i = 0; i < QB; ++i) {
+                        for (int q = 0; q < YP; ++q) fm[q] = *(const bf16x8 *)m_at(sm, q, m_row(16 * i + col) + 32 * k + 8 * g);
+                        sum = mma_parts<YP>(fx[k], fm, sum);
+                    }
+                    if (__any(odd[0] != 0.0f || odd[1] != 0.0f || odd[2] != 0.0f || odd[3] != 0.0f)) {
                         const int t = 16 * i + col;
+                        sum = acc[i];
+#pragma unroll 1
                         for (int s = 0; s <= t; ++s) {
                             float m = 0.0f;
 #pragma unroll
-                            for (int q = 0; q < YP; ++q) m += (float)*m_at(sm, q, lds_at<QCH>(t, s >> 3) + (s & 7));
+                            for (int q = 0; q < YP; ++q) m += (float)*m_at(sm, q, m_row(t) + s);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 float x = 0.0f;
 #pragma unroll
-                                for (int q = 0; q < NP; ++q)
-                                    x += (float)sm.xt[q][lds_at<QCH>(wave * 16 + 4 * g + j, s >> 3) + (s & 7)];
-                                acc[i][j] = fmaf(m, x, acc[i][j]);
+                                for (int q = 0; q < NP; ++q) x += (float)sm.xt[q][(wave * 16 + 4 * g + j) * kS + s];
+                                sum[j] = fmaf(m, x, sum[j]);
                             }
                         }
                     }
+                    acc[i] = sum;
                 }
+                const Rows yrows = rows_at(a.y + (int64_t)(first + t0) * a.y_stride + hp);
+                const uint32_t ys = (uint32_t)a.y_stride * e;
 #pragma unroll
                 for (int i = 0; i < QB; ++i) {
-                    const int t = t0 + 16 * i + col;
-                    if (t >= length || p4 >= P) continue;
-                    T *const yp = a.y + (int64_t)(first + t) * a.y_stride + hp + p4;
-                    Raw<T, 4> out;
+                    Piece<T, 4> out;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float v = acc[i][j];
                         if (a.z) v *= silu_as<T>((float)rz[i].v[j]);
                         out.v[j] = (T)v;
                     }
-                    if (a.vec_y) *(typename Raw<T, 4>::vec *)yp = out.v;
-                    else
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (p4 + j < P) yp[j] = out.v[j];
+                    out.template store<WIDE>(yrows, col * ys + p4 * e, 16 * i * ys, t0 + 16 * i + col < length ? P - p4 : 0);
                 }
             }
 
@@ -463,17 +493,11 @@ template <typename T, int NPAD, int Q, bool FULL> struct SsmScan {
             bf16x8 fw[QK][3];
 #pragma unroll
             for (int k = 0; k < QK; ++k) {
-                const f32x4 w0 = *(const f32x4 *)&sm.into[32 * k + 8 * g], w1 = *(const f32x4 *)&sm.into[32 * k + 8 * g + 4];
+                const f32x4 w0 = *(const f32x4 *)&sc.into[32 * k + 8 * g], w1 = *(const f32x4 *)&sc.into[32 * k + 8 * g + 4];
+                f32x8 x = __builtin_convertvector(fx[k][NP - 1], f32x8);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    float x = 0.0f;
-#pragma unroll
-                    for (int q = NP - 1; q >= 0; --q) x += (float)fx[k][q][j];
-                    bf16 u[3];
-                    split<3>(x * (j < 4 ? w0[j & 3] : w1[j & 3]), u);
-#pragma unroll
-                    for (int q = 0; q < 3; ++q) fw[k][q][j] = u[q];
-                }
+                for (int q = NP - 2; q >= 0; --q) x += __builtin_convertvector(fx[k][q], f32x8);
+                split(x * __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7), fw[k]);
             }
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
@@ -482,7 +506,7 @@ template <typename T, int NPAD, int Q, bool FULL> struct SsmScan {
                 for (int k = 0; k < QK; ++k) {
                     bf16x8 fb[NP];
 #pragma unroll
-                    for (int q = 0; q < NP; ++q) fb[q] = *(const bf16x8 *)&sm.bt[q][lds_at<QCH>(16 * i + col, 4 * k + g)];
+                    for (int q = 0; q < NP; ++q) fb[q] = *(const bf16x8 *)&sm.bt[q][(16 * i + col) * kS + 32 * k + 8 * g];
                     h[i] = mma_parts<3>(fb, fw[k], h[i]);
                 }
             }
@@ -497,10 +521,11 @@ template <typename T, int NPAD, int Q, bool FULL> struct SsmScan {
     }
 };
 
-template <typename T, int NPAD, int Q, bool FULL> __global__ void __launch_bounds__(256, (sizeof(typename SsmScan<T, NPAD, Q, FULL>::Shared) > 81920 ? 1 : 2))
+template <typename T, int NPAD, int Q, bool FULL, bool WIDE>
+__global__ void __launch_bounds__(256, (sizeof(typename SsmScan<T, NPAD, Q, FULL, WIDE>::Shared) > 81920 ? 1 : 2))
 ssm_scan_kernel(SsmArgs<T> a)
 {
-    typedef SsmScan<T, NPAD, Q, FULL> Scan;
+    typedef SsmScan<T, NPAD, Q, FULL, WIDE> Scan;
     __shared__ typename Scan::Shared sm;
     Scan::run(a, sm);
 }
