@@ -60,7 +60,7 @@ template <typename T, int V, int W> __global__ void __launch_bounds__(256) causa
 
     if (head) {
         const int slot = request_slot(a.rq, blockIdx.y);
-        const bool resume = a.state_in && slot >= 0 && (!a.rq.resume || a.rq.resume[blockIdx.y] != 0);
+        const bool resume = a.state_in && slot >= 0 && request_resumes(a.rq, blockIdx.y);
         const size_t at = (size_t)max(slot, 0) * (W - 1) * a.channels + c;
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {

@@ -45,6 +45,48 @@ __device__ inline float silu_fast(float v)
 template <typename T> __device__ inline float silu_as(float v) { return sizeof(T) == 4 ? silu(v) : silu_fast(v); }
 __device__ inline float softplus(float v) { return fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v))); }
 
+// log(1 + e) as log(u) e / (u - 1) with u = 1 + e rounded (Goldberg 1991, theorem 4): the quotient makes up for what the
+// rounding lost, so the result is good to a few units of the last place however small e is
+__device__ inline float softplus_fast(float v)
+{
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(v)), u = 1.0f + e, d = u - 1.0f;
+    const float l = d == 0.0f ? e : 0.69314718f * __builtin_amdgcn_logf(u) * (e * __builtin_amdgcn_rcpf(d));
+    return fmaxf(v, 0.0f) + l;
+}
+
+// ---- sums over the lanes before, in 64 bits: data moves within rows of 16 lanes and then from row ends on -----------
+template <int CTRL, int ROWS> __device__ inline double lanes_before(double v)      // zero where there is none
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ inline double running_sum(double v)
+{
+    v += lanes_before<0x111, 0xf>(v);     // row_shr 1, 2, 4, 8
+    v += lanes_before<0x112, 0xf>(v);
+    v += lanes_before<0x114, 0xf>(v);
+    v += lanes_before<0x118, 0xf>(v);
+    v += lanes_before<0x142, 0xa>(v);     // lane 15 of a row to the next row: into rows 1 and 3
+    v += lanes_before<0x143, 0xc>(v);     // lane 31 to the next two rows: into rows 2 and 3
+    return v;
+}
+
+__device__ inline double read_lane(double v, int lane)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// what the last lane of a lane's row of 16 holds
+__device__ inline double row_end(double v)
+{
+    const double e0 = read_lane(v, 15), e1 = read_lane(v, 31), e2 = read_lane(v, 47), e3 = read_lane(v, 63);
+    const int row = (threadIdx.x >> 4) & 3;
+    return row < 2 ? (row == 0 ? e0 : e1) : (row == 2 ? e2 : e3);
+}
+
 template <typename T> __device__ inline float apply_act(float v, int act)
 {
     if (act == WPK_ACT_RELU) return v < 0.0f ? 0.0f : v;                  // (NaN stays)
@@ -55,75 +97,55 @@ template <typename T> __device__ inline float apply_act(float v, int act)
 
 // ---- rows through buffer descriptors: what is outside a tensor reads as zero and is not written, without a branch -----
 typedef __amdgpu_buffer_rsrc_t Rows;
-static const uint32_t kOutside = 0x80000000u;    // an offset that no descriptor reaches
-__device__ inline Rows rows_at(const void *base)
+static const uint32_t kOutside = 0x80000000u;    // an offset that no descriptor reaches, nor with a tile's rows added
+// `rows` rows (none where that is negative) of `stride` bytes, together below 2^31
+__device__ inline Rows rows_at(const void *base, int rows, uint32_t stride)
 {
-    return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, __builtin_amdgcn_readfirstlane(max(rows, 0)) * stride, 0x00020000);
 }
 
-// V elements of a row, `left` of them there (none if the row is not): at once, or one by one where rows are not aligned
+// V elements of a row from `offset` on, of which `left` are there.  Rows that are aligned are moved at once: all V are there
+// or, with an offset that is outside, none.
 template <typename T, int V> struct Piece {
     static const int words = V * (int)sizeof(T) / 4;
     typedef T vec_t __attribute__((ext_vector_type(V)));
     vec_t v;
 
-    // (`step`: bytes that are the same for all lanes)
-    template <bool WIDE> __device__ void load(Rows rows, uint32_t offset, uint32_t step, int left)
+    template <bool WIDE> __device__ void load(Rows rows, uint32_t offset, int left)
     {
-        if constexpr (WIDE) {
-            const uint32_t at = left > 0 ? offset : kOutside;
-            union {
-                uint32_t w[words];
-                vec_t v;
+        if constexpr (WIDE && words == 2) {
+            v = __builtin_bit_cast(vec_t, __builtin_amdgcn_raw_buffer_load_b64(rows, offset, 0, 0));
+        } else if constexpr (WIDE && words == 4) {
+            v = __builtin_bit_cast(vec_t, __builtin_amdgcn_raw_buffer_load_b128(rows, offset, 0, 0));
+        } else if constexpr (WIDE) {
+            struct {
+                u32x4 q[words / 4];
             } u;
-            if constexpr (words >= 4) {
 #pragma unroll
-                for (int i = 0; i < words; i += 4) {
-                    const u32x4 q = __builtin_amdgcn_raw_buffer_load_b128(rows, at + 4 * i, step, 0);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) u.w[i + j] = q[j];
-                }
-            } else {
-                const u32x2 q = __builtin_amdgcn_raw_buffer_load_b64(rows, at, step, 0);
-                u.w[0] = q[0];
-                u.w[1] = q[1];
-            }
-            v = u.v;
+            for (int i = 0; i < words / 4; ++i) u.q[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, offset + 16 * i, 0, 0);
+            v = __builtin_bit_cast(vec_t, u);
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const uint32_t at = i < left ? offset + i * (uint32_t)sizeof(T) : kOutside;
-                if constexpr (sizeof(T) == 2) v[i] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rows, at, step, 0));
-                else v[i] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(rows, at, step, 0));
+                if constexpr (sizeof(T) == 2) v[i] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rows, at, 0, 0));
+                else v[i] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(rows, at, 0, 0));
             }
         }
     }
 
-    template <bool WIDE> __device__ void store(Rows rows, uint32_t offset, uint32_t step, int left) const
+    template <bool WIDE> __device__ void store(Rows rows, uint32_t offset, int left) const
     {
-        if constexpr (WIDE) {
-            const uint32_t at = left > 0 ? offset : kOutside;
-            union {
-                uint32_t w[words];
-                vec_t v;
-            } u;
-            u.v = v;
-            if constexpr (words >= 4) {
-#pragma unroll
-                for (int i = 0; i < words; i += 4) {
-                    u32x4 q = {u.w[i], u.w[i + 1], u.w[i + 2], u.w[i + 3]};
-                    __builtin_amdgcn_raw_buffer_store_b128(q, rows, at + 4 * i, step, 0);
-                }
-            } else {
-                u32x2 q = {u.w[0], u.w[1]};
-                __builtin_amdgcn_raw_buffer_store_b64(q, rows, at, step, 0);
-            }
+        if constexpr (WIDE && words == 2) {
+            __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), rows, offset, 0, 0);
+        } else if constexpr (WIDE && words == 4) {
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rows, offset, 0, 0);
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const uint32_t at = i < left ? offset + i * (uint32_t)sizeof(T) : kOutside;
-                if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)v[i]), rows, at, step, 0);
-                else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, (T)v[i]), rows, at, step, 0);
+                if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)v[i]), rows, at, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, (T)v[i]), rows, at, 0, 0);
             }
         }
     }
@@ -135,13 +157,13 @@ struct Requests {
     int32_t tokens, max_length, slots;
 };
 
-// rows [first, first + length) of request i
+// rows [first, first + length) of request i, the same for all lanes as i is (and known to be)
 __device__ inline void request_rows(const Requests &q, int i, int *first, int *length)
 {
     if (q.starts) {
         const int a = min(max(q.starts[i], 0), q.tokens), b = min(max(q.starts[i + 1], 0), q.tokens);
-        *first = a;
-        *length = max(b - a, 0);
+        *first = __builtin_amdgcn_readfirstlane(a);
+        *length = __builtin_amdgcn_readfirstlane(max(b - a, 0));
     } else {
         *first = i * q.max_length;
         *length = q.max_length;
@@ -151,8 +173,13 @@ __device__ inline void request_rows(const Requests &q, int i, int *first, int *l
 // entry of request i's state, or -1
 __device__ inline int request_slot(const Requests &q, int i)
 {
-    const int s = q.slot_map ? q.slot_map[i] : i;
+    const int s = q.slot_map ? __builtin_amdgcn_readfirstlane(q.slot_map[i]) : i;
     return s >= 0 && s < q.slots ? s : -1;
+}
+
+__device__ inline bool request_resumes(const Requests &q, int i)
+{
+    return !q.resume || __builtin_amdgcn_readfirstlane(q.resume[i]) != 0;
 }
 
 // What the two kinds of call check alike; `step` for the calls of one token a request.

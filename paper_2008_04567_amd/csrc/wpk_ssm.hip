@@ -19,7 +19,7 @@ template <typename T, int V, int CI, int U> __global__ void __launch_bounds__(25
     const int p0 = blockIdx.z * U * rows + (threadIdx.x >> lpr_log);
     int first, length;
     request_rows(a.rq, r, &first, &length);
-    const int slot = __builtin_amdgcn_readfirstlane(request_slot(a.rq, r));
+    const int slot = request_slot(a.rq, r);
     const bool resume = a.state_in && slot >= 0, leave = a.state_out && slot >= 0;
     const size_t at = ((size_t)max(slot, 0) * a.heads + head) * P * N;
     const float *const in = a.state_in + at;
@@ -34,8 +34,8 @@ template <typename T, int V, int CI, int U> __global__ void __launch_bounds__(25
             if (resume && p < P && n < N) h[u][i] = __builtin_nontemporal_load((const vec *)(in + (unsigned)(p * N + n)));
         }
     const int group = head / (a.heads / a.groups);
-    const Rows brows = rows_at(a.b + (int64_t)first * a.b_stride + group * N);
-    const Rows crows = rows_at(a.c + (int64_t)first * a.c_stride + group * N);
+    const Rows brows = rows_at(a.b + (int64_t)first * a.b_stride + group * N, 1, N * (uint32_t)sizeof(T));
+    const Rows crows = rows_at(a.c + (int64_t)first * a.c_stride + group * N, 1, N * (uint32_t)sizeof(T));
     const T *const xp = a.x + (int64_t)first * a.x_stride + (int64_t)head * P;
     const T *const zp = a.z + (int64_t)first * a.z_stride + (int64_t)head * P;
     T *const yp = a.y + (int64_t)first * a.y_stride + (int64_t)head * P;
@@ -44,8 +44,8 @@ template <typename T, int V, int CI, int U> __global__ void __launch_bounds__(25
 #pragma unroll
     for (int i = 0; i < CI; ++i) {
         const int n = at_n + i * V * lpr;
-        b[i].template load<V == 4>(brows, n * (uint32_t)sizeof(T), 0, N - n);
-        c[i].template load<V == 4>(crows, n * (uint32_t)sizeof(T), 0, N - n);
+        b[i].template load<V == 4>(brows, n * (uint32_t)sizeof(T), N - n);
+        c[i].template load<V == 4>(crows, n * (uint32_t)sizeof(T), N - n);
     }
     T x[U], z[U];
 #pragma unroll

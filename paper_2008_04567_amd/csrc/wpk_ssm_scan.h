@@ -57,6 +57,16 @@ template <int LIMIT, int PA, int PB> __device__ inline f32x4 mma_parts(const bf1
     return c;
 }
 
+// the pairs that mma_parts takes, one by one, for products that are better interleaved
+template <int LIMIT, int PA, int PB, typename F> __device__ inline void each_pair(F f)
+{
+#pragma unroll
+    for (int i = 0; i < PA; ++i)
+#pragma unroll
+        for (int j = 0; j < PB; ++j)
+            if (i + j < LIMIT) f(i, j);
+}
+
 // values as sums of parts, the largest first
 template <typename BF, int PARTS, typename F> __device__ inline void split(F v, BF (&out)[PARTS])
 {
@@ -98,7 +108,8 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
     static __device__ int m_row(int t) { return Q == 64 ? (t < 32 ? t * 40 : t * kS - 32 * (kS - 40)) : t * kS; }
 
     struct alignas(16) Scalars {
-        alignas(16) float sh[Q], sl[Q], delta[Q], into[Q], from[Q];   // S in two floats, delta, exp(S_end - S) delta, exp(S)
+        // S in two floats, delta, exp(S_end - S) delta, exp(S), exp(S_e - S) delta with e the end of a token's block of 16
+        alignas(16) float sh[Q], sl[Q], delta[Q], into[Q], from[Q], block[Q];
         float keep[4];
     };
     struct alignas(16) Shared {
@@ -144,7 +155,7 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
 
         const int p_base = pblock * 64, p = p_base + wave * 16 + col;   // p: the state row whose columns this lane holds
         const int slot = request_slot(a.rq, r);
-        const bool resume = a.state_in && slot >= 0 && (!a.rq.resume || a.rq.resume[r] != 0);
+        const bool resume = a.state_in && slot >= 0 && request_resumes(a.rq, r);
         const size_t state_size = (size_t)P * N, row_at = (size_t)min(p, P - 1) * N;
         const size_t pool_at = ((size_t)max(slot, 0) * a.heads + head) * state_size + row_at;
         const size_t ws_head = (size_t)r * a.heads + head;
@@ -185,16 +196,13 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
         // The state before the part.  Parts meet through the workspace: entry i holds what part i's tokens leave (part 0's
         // with the state before the request), the last entry the state before the request itself, since whoever does the
         // last part may be writing the pool's entry already.
-        bool zero_state = true;
         if (part == 0) {
             if (resume) {
                 add_state(FULL && parts > 1 ? ws + (size_t)(a.n_parts - 1) * state_size : a.state_in + pool_at, 0.0f);
-                zero_state = false;
                 if (!FULL) put_state(ws + (size_t)(a.n_parts - 1) * state_size);
             }
         } else if (FULL) {
             for (int i = 0; i < part; ++i) add_state(ws + (size_t)i * state_size, i ? a.part_decay[ws_head * a.n_parts + i] : 0.0f);
-            zero_state = false;
         }
 
         const float rate = a.a[head], skip = a.d_skip ? a.d_skip[head] : 0.0f, dt_bias = a.dt_bias ? a.dt_bias[head] : 0.0f;
@@ -206,19 +214,20 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
         Piece<T, 4> rx[kXPer][4];
         const uint32_t e = sizeof(T);
         const uint32_t bs = (uint32_t)a.b_stride * e, cs = (uint32_t)a.c_stride * e, xs = (uint32_t)a.x_stride * e;
-        auto fetch = [&](int chunk) {
-            const int t0 = chunk * Q, left = length - t0;       // rows that there are
-            const Rows brows = rows_at(bp + (int64_t)t0 * a.b_stride), crows = rows_at(cp + (int64_t)t0 * a.c_stride);
-            const Rows xrows = rows_at(xp + (int64_t)t0 * a.x_stride);
+        const uint32_t zs = (uint32_t)a.z_stride * e, ys = (uint32_t)a.y_stride * e;
+        auto fetch = [&](int chunk, bool want_b, bool want_c, bool want_x) {
+            const int t0 = chunk * Q, left = min(length - t0, Q);       // rows that there are
+            const Rows brows = rows_at(bp + (int64_t)t0 * a.b_stride, left, bs), crows = rows_at(cp + (int64_t)t0 * a.c_stride, left, cs);
+            const Rows xrows = rows_at(xp + (int64_t)t0 * a.x_stride, left, xs);
 #pragma unroll
             for (int i = 0; i < kBPer; ++i) {
                 int s, n;
                 b_task(tid + 256 * i, &s, &n);
+                const uint32_t out = 8 * n < N && s < Q ? 0 : kOutside;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int cols = s + j < left ? N - 8 * n : 0;
-                    rb[i][j].template load<WIDE>(brows, s * bs + n * 8 * e, j * bs, cols);
-                    if (FULL) rc[i][j].template load<WIDE>(crows, s * cs + n * 8 * e, j * cs, cols);
+                    if (want_b) rb[i][j].template load<WIDE>(brows, (s * bs + n * 8 * e | out) + j * bs, N - 8 * n);
+                    if (FULL && want_c) rc[i][j].template load<WIDE>(crows, (s * cs + n * 8 * e | out) + j * cs, N - 8 * n);
                 }
             }
 #pragma unroll
@@ -226,9 +235,10 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
                 int s, q;
                 x_task(tid + 256 * i, &s, &q);
                 q = p_base + 4 * q;
+                const uint32_t out = q < P ? 0 : kOutside;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    rx[i][j].template load<WIDE>(xrows, s * xs + q * e, j * xs, s + j < left ? P - q : 0);
+                    if (want_x) rx[i][j].template load<WIDE>(xrows, (s * xs + q * e | out) + j * xs, P - q);
             }
         };
         auto stage = [&]() {
@@ -296,39 +306,34 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
         auto fetch_dt = [&](int chunk) {
             const int t0 = chunk * Q;
             Piece<T, 1> d;
-            d.template load<false>(rows_at(dtp + (int64_t)t0 * a.dt_stride), lane * (uint32_t)a.dt_stride * e, 0,
-                                   lane < Q && t0 + lane < length ? 1 : 0);
+            const uint32_t ds = (uint32_t)a.dt_stride * e;
+            d.template load<false>(rows_at(dtp + (int64_t)t0 * a.dt_stride, min(length - t0, Q), ds), lane * ds, 1);
             rdt = (float)d.v[0];
         };
         auto scalars = [&](int chunk) {
             Scalars &sc = sm.sc[chunk & (kSc - 1)];
             const bool live = lane < Q && chunk * Q + lane < length;
             float delta = rdt + dt_bias;
-            if (a.softplus) delta = softplus(delta);
+            if (a.softplus) delta = softplus_fast(delta);
             if (!live) delta = 0.0f;
             double s = (double)delta * rate * 1.4426950408889634;
-            if (s < -192.0) s = -192.0;
-            if (!live) s = 0.0;
-#pragma unroll
-            for (int m = 1; m < Q; m <<= 1) {
-                const double o = __shfl_up(s, m);
-                if (lane >= m) s += o;
-            }
-            const double end = __shfl(s, Q - 1);
+            s = running_sum(!live ? 0.0 : s < -192.0 ? -192.0 : s);
+            const double end = read_lane(s, Q - 1);
             if (lane < Q) {
                 sc.sh[lane] = (float)s;
                 sc.sl[lane] = (float)(s - (double)(float)s);
                 sc.delta[lane] = delta;
                 sc.into[lane] = delta * __builtin_amdgcn_exp2f((float)(end - s));
                 sc.from[lane] = __builtin_amdgcn_exp2f((float)s);
+                sc.block[lane] = delta * __builtin_amdgcn_exp2f((float)(row_end(s) - s));
             }
             if (lane == 0) sc.keep[0] = __builtin_amdgcn_exp2f((float)end);
         };
-        const int kScalarWave = 3;
+        const int kScalarWave = 0;
 
         float total = 1.0f;
         if (c0 < c1) {
-            fetch(c0);
+            fetch(c0, true, true, true);
             if (wave == kScalarWave) {
                 fetch_dt(c0);
                 scalars(c0);
@@ -336,7 +341,23 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
             }
         }
         const int p4 = p_base + wave * 16 + 4 * g;      // rows of y that this lane stores
+        const uint32_t out4 = p4 < P ? 0 : kOutside;
         const bf16x8 zero8 = {0, 0, 0, 0, 0, 0, 0, 0};
+        // This wave's 16 x 16 blocks of M: one on the diagonal and up to two below it (rows 1 .. 3 of four share six).  Blocks
+        // above it in a row's 32 columns stay zero.
+        const int tb0 = Q == 64 ? wave : wave & 1;
+        const int tb1 = Q == 64 ? (wave == 0 ? 3 : wave) : 1, sb1 = Q == 64 ? (wave == 0 ? 0 : wave - 1) : 0;
+        const int tb2 = wave == 1 ? 2 : 3, sb2 = wave == 1 ? 0 : 1;
+        const bool has0 = Q == 64 || wave < 2, has1 = Q == 64 || wave == 2, has2 = Q == 64 && (wave & 1);
+        auto zero_blocks = [&]() {
+            if (wave == (Q == 64 ? 0 : 3) || (Q == 64 && wave == 2)) {
+                const int t = 16 * (Q == 64 ? wave : 0) + col, s0 = 16 * (Q == 64 ? wave + 1 : 1) + 4 * g;
+                const bf16x4 w = {0, 0, 0, 0};
+#pragma unroll
+                for (int q = 0; q < YP; ++q) *(bf16x4 *)m_at(sm, q, m_row(t) + s0) = w;
+            }
+        };
+        if (FULL && !kAlias) zero_blocks();
         for (int chunk = c0; chunk < c1; ++chunk) {
             stage();
             if (kTight && chunk > c0 && wave == kScalarWave) {
@@ -344,94 +365,101 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
                 fetch_dt(chunk + 1);
             }
             __syncthreads();
-            const int t0 = chunk * Q;
+            const int t0 = chunk * Q, left = min(length - t0, Q);
             const Scalars &sc = sm.sc[chunk & (kSc - 1)];
             Piece<T, 4> rz[FULL ? QB : 1];
             if (FULL && a.z) {
-                const Rows zrows = rows_at(a.z + (int64_t)(first + t0) * a.z_stride + hp);
-                const uint32_t zs = (uint32_t)a.z_stride * e;
+                const Rows zrows = rows_at(a.z + (int64_t)(first + t0) * a.z_stride + hp, left, zs);
 #pragma unroll
                 for (int i = 0; i < QB; ++i)
-                    rz[i].template load<WIDE>(zrows, col * zs + p4 * e, 16 * i * zs, t0 + 16 * i + col < length ? P - p4 : 0);
+                    rz[i].template load<WIDE>(zrows, (col * zs + p4 * e | out4) + 16 * i * zs, P - p4);
             }
-            if (chunk + 1 < c1) fetch(chunk + 1);
+            const int next = min(chunk + 1, c1 - 1);       // (the last chunk again behind the last)
+            fetch(next, true, false, !FULL);
             const float keep = sc.keep[0];
             total *= keep;
 
             f32x4 acc[FULL ? QB : 1];
             if (FULL) {
                 // G transposed, block by block (rows s, column t in the lane), into M
-                f32x4 gt[kPerWave];
-#pragma unroll
-                for (int i = 0; i < kPerWave; ++i) {
-                    const int k = wave + 4 * i, tb = k < 4 ? k >> 1 : 2 + ((k - 4) >> 2), sb = k < 4 ? k & 1 : (k - 4) & 3;
-                    gt[i] = f32x4{0, 0, 0, 0};
-                    if (sb > tb) continue;
-                    const int at_b = (16 * sb + col) * kN + 8 * g, at_c = (16 * tb + col) * kN + 8 * g;
+                f32x4 g0 = {0, 0, 0, 0}, g1 = g0, g2 = g0;
+                auto block = [&](int t, int u, f32x4 sum) {
 #pragma unroll
                     for (int n = 0; n < NPAD / 32; ++n) {
                         bf16x8 fb[NP], fc[NP];
 #pragma unroll
                         for (int q = 0; q < NP; ++q) {
-                            fb[q] = *(const bf16x8 *)&sm.b[q][at_b + 32 * n];
-                            fc[q] = *(const bf16x8 *)&sm.c[q][at_c + 32 * n];
+                            fb[q] = *(const bf16x8 *)&sm.b[q][(16 * u + col) * kN + 8 * g + 32 * n];
+                            fc[q] = *(const bf16x8 *)&sm.c[q][(16 * t + col) * kN + 8 * g + 32 * n];
                         }
-                        gt[i] = mma_parts<NP>(fb, fc, gt[i]);
+                        sum = mma_parts<NP>(fb, fc, sum);
                     }
-                }
-                if (kAlias) __syncthreads();
-#pragma unroll
-                for (int i = 0; i < kPerWave; ++i) {
-                    const int k = wave + 4 * i, tb = k < 4 ? k >> 1 : 2 + ((k - 4) >> 2), sb = k < 4 ? k & 1 : (k - 4) & 3;
-                    const int t = 16 * tb + col, s0 = 16 * sb + 4 * g;
-                    f32x4 v = {0, 0, 0, 0};
-                    if (sb <= tb) {
-                        const f32x4 sh = *(const f32x4 *)&sc.sh[s0], sl = *(const f32x4 *)&sc.sl[s0];
-                        const f32x4 dl = *(const f32x4 *)&sc.delta[s0];
-                        const float th = sc.sh[t], tl = sc.sl[t];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            v[j] = gt[i][j] * (__builtin_amdgcn_exp2f((th - sh[j]) + (tl - sl[j])) * dl[j]);
-                        if (sb == tb)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) v[j] = s0 + j > t ? 0.0f : s0 + j == t ? v[j] + skip : v[j];
-                    }
+                    return sum;
+                };
+                auto put_block = [&](int t, int s0, f32x4 v) {
                     bf16x4 w[YP];
                     split(v, w);
 #pragma unroll
                     for (int q = 0; q < YP; ++q) *(bf16x4 *)m_at(sm, q, m_row(t) + s0) = w[q];
+                };
+                // below the diagonal exp(S_t - S_s) is exp(S_t - S_e) exp(S_e - S_s), e the last token of the column's block
+                auto below = [&](int tb, int sb, f32x4 v) {
+                    const int t = 16 * tb + col, s0 = 16 * sb + 4 * g, end = 16 * sb + 15;
+                    const float u = __builtin_amdgcn_exp2f((sc.sh[t] - sc.sh[end]) + (sc.sl[t] - sc.sl[end]));
+                    put_block(t, s0, v * (*(const f32x4 *)&sc.block[s0] * u));
+                };
+                if (has0) g0 = block(tb0, tb0, g0);
+                if (has1) g1 = block(tb1, sb1, g1);
+                if (has2) g2 = block(tb2, sb2, g2);
+                if (kAlias) {
+                    __syncthreads();
+                    zero_blocks();
                 }
+                if (has0) {
+                    const int t = 16 * tb0 + col, s0 = 16 * tb0 + 4 * g;
+                    const f32x4 sh = *(const f32x4 *)&sc.sh[s0], sl = *(const f32x4 *)&sc.sl[s0];
+                    const f32x4 dl = *(const f32x4 *)&sc.delta[s0];
+                    const float th = sc.sh[t], tl = sc.sl[t];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        g0[j] *= __builtin_amdgcn_exp2f((th - sh[j]) + (tl - sl[j])) * dl[j];
+                        g0[j] = 4 * g + j > col ? 0.0f : 4 * g + j == col ? g0[j] + skip : g0[j];
+                    }
+                    put_block(t, s0, g0);
+                }
+                if (has1) below(tb1, sb1, g1);
+                if (has2) below(tb2, sb2, g2);
+                fetch(next, false, true, false);
                 // exp(S) C h0: rows p, column t in the lane
 #pragma unroll
                 for (int i = 0; i < QB; ++i) acc[i] = f32x4{0, 0, 0, 0};
-                if (!zero_state || chunk > c0) {
 #pragma unroll
-                    for (int n = 0; n < NPAD / 32; ++n) {
-                        bf16x8 fh[YP];
-                        split(__builtin_shufflevector(h[2 * n], h[2 * n + 1], 0, 1, 2, 3, 4, 5, 6, 7), fh);
+                for (int n = 0; n < NPAD / 32; ++n) {
+                    bf16x8 fh[YP], fc[QB][NP];
+                    split(__builtin_shufflevector(h[2 * n], h[2 * n + 1], 0, 1, 2, 3, 4, 5, 6, 7), fh);
 #pragma unroll
-                        for (int i = 0; i < QB; ++i) {
-                            bf16x8 fc[NP];
+                    for (int i = 0; i < QB; ++i)
 #pragma unroll
-                            for (int q = 0; q < NP; ++q) {
-                                const bf16 *const at = &sm.c[q][(16 * i + col) * kN + 32 * n + 4 * g];
-                                const bf16x4 lo = *(const bf16x4 *)at, hi = *(const bf16x4 *)(at + 16);
-                                fc[q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                            }
-                            acc[i] = mma_parts<YP>(fh, fc, acc[i]);
+                        for (int q = 0; q < NP; ++q) {
+                            const bf16 *const at = &sm.c[q][(16 * i + col) * kN + 32 * n + 4 * g];
+                            const bf16x4 lo = *(const bf16x4 *)at, hi = *(const bf16x4 *)(at + 16);
+                            fc[i][q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                         }
-                    }
+                    each_pair<YP, YP, NP>([&](int u, int v) {
 #pragma unroll
-                    for (int i = 0; i < QB; ++i) acc[i] *= sc.from[16 * i + col];
+                        for (int i = 0; i < QB; ++i) acc[i] = mma(fh[u], fc[i][v], acc[i]);
+                    });
                 }
-                if (!kTight && wave == kScalarWave && chunk + 1 < c1) {
-                    scalars(chunk + 1);
-                    fetch_dt(chunk + 2);
-                }
-                __syncthreads();
-            } else if (!kTight && wave == kScalarWave && chunk + 1 < c1) {
+#pragma unroll
+                for (int i = 0; i < QB; ++i) acc[i] *= sc.from[16 * i + col];
+            }
+            if (!kTight && wave == kScalarWave && chunk + 1 < c1) {
                 scalars(chunk + 1);
                 fetch_dt(chunk + 2);
+            }
+            if (FULL) {
+                __syncthreads();
+                fetch(next, false, false, true);
             }
 
             bf16x8 fx[QK][NP];
@@ -439,25 +467,58 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
             for (int k = 0; k < QK; ++k)
 #pragma unroll
                 for (int q = 0; q < NP; ++q) fx[k][q] = *(const bf16x8 *)&sm.xt[q][(wave * 16 + col) * kS + 32 * k + 8 * g];
-
-            if (FULL) {
-                // Infinities or NaN among x may not meet the zeros of M that stand for later tokens: x times zero finds them.
-                f32x4 odd = {0, 0, 0, 0};
+            // Infinities or NaN among x may not meet the zeros of M that stand for later tokens: x times zero finds them.
+            f32x4 odd = {0, 0, 0, 0};
+            if (FULL)
 #pragma unroll
                 for (int k = 0; k < QK; ++k) odd = mma(fx[k][0], zero8, odd);
+
+            // the state behind the chunk
 #pragma unroll
-                for (int i = 0; i < QB; ++i) {
-                    f32x4 sum = acc[i];
+            for (int i = 0; i < NB; ++i) h[i] *= keep;
 #pragma unroll
-                    for (int k = 0; k <= i / 2; ++k) {
-                        bf16x8 fm[YP];
+            for (int k = 0; k < QK; ++k) {
+                const f32x4 w0 = *(const f32x4 *)&sc.into[32 * k + 8 * g], w1 = *(const f32x4 *)&sc.into[32 * k + 8 * g + 4];
+                f32x8 x = __builtin_convertvector(fx[k][NP - 1], f32x8);
 #pragma unroll
-                        for (int q = 0; q < YP; ++q) fm[q] = *(const bf16x8 *)m_at(sm, q, m_row(16 * i + col) + 32 * k + 8 * g);
-                        sum = mma_parts<YP>(fx[k], fm, sum);
+                for (int q = NP - 2; q >= 0; --q) x += __builtin_convertvector(fx[k][q], f32x8);
+                bf16x8 fw[3];
+                split(x * __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7), fw);
+                const int kStep = NB * NP > 16 ? NB / 2 : NB;      // blocks of the state that go side by side
+#pragma unroll
+                for (int i0 = 0; i0 < NB; i0 += kStep) {
+                    bf16x8 fb[kStep][NP];
+#pragma unroll
+                    for (int i = 0; i < kStep; ++i)
+#pragma unroll
+                        for (int q = 0; q < NP; ++q)
+                            fb[i][q] = *(const bf16x8 *)&sm.bt[q][(16 * (i0 + i) + col) * kS + 32 * k + 8 * g];
+                    each_pair<3, NP, 3>([&](int u, int v) {
+#pragma unroll
+                        for (int i = 0; i < kStep; ++i) h[i0 + i] = mma(fb[i][u], fw[v], h[i0 + i]);
+                    });
+                }
+            }
+
+            if (FULL) {
+                if (!__any(odd[0] != 0.0f || odd[1] != 0.0f || odd[2] != 0.0f || odd[3] != 0.0f)) {
+#pragma unroll
+                    for (int k = 0; k < QK; ++k) {
+                        bf16x8 fm[QB][YP];
+#pragma unroll
+                        for (int i = 2 * k; i < QB; ++i)
+#pragma unroll
+                            for (int q = 0; q < YP; ++q)
+                                fm[i][q] = *(const bf16x8 *)m_at(sm, q, m_row(16 * i + col) + 32 * k + 8 * g);
+                        each_pair<YP, NP, YP>([&](int u, int v) {
+#pragma unroll
+                            for (int i = 2 * k; i < QB; ++i) acc[i] = mma(fx[k][u], fm[i][v], acc[i]);
+                        });
                     }
-                    if (__any(odd[0] != 0.0f || odd[1] != 0.0f || odd[2] != 0.0f || odd[3] != 0.0f)) {
+                } else {
+#pragma unroll
+                    for (int i = 0; i < QB; ++i) {
                         const int t = 16 * i + col;
-                        sum = acc[i];
 #pragma unroll 1
                         for (int s = 0; s <= t; ++s) {
                             float m = 0.0f;
@@ -468,14 +529,12 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
                                 float x = 0.0f;
 #pragma unroll
                                 for (int q = 0; q < NP; ++q) x += (float)sm.xt[q][(wave * 16 + 4 * g + j) * kS + s];
-                                sum[j] = fmaf(m, x, sum[j]);
+                                acc[i][j] = fmaf(m, x, acc[i][j]);
                             }
                         }
                     }
-                    acc[i] = sum;
                 }
-                const Rows yrows = rows_at(a.y + (int64_t)(first + t0) * a.y_stride + hp);
-                const uint32_t ys = (uint32_t)a.y_stride * e;
+                const Rows yrows = rows_at(a.y + (int64_t)(first + t0) * a.y_stride + hp, left, ys);
 #pragma unroll
                 for (int i = 0; i < QB; ++i) {
                     Piece<T, 4> out;
@@ -485,29 +544,7 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
                         if (a.z) v *= silu_as<T>((float)rz[i].v[j]);
                         out.v[j] = (T)v;
                     }
-                    out.template store<WIDE>(yrows, col * ys + p4 * e, 16 * i * ys, t0 + 16 * i + col < length ? P - p4 : 0);
-                }
-            }
-
-            // the state behind the chunk
-            bf16x8 fw[QK][3];
-#pragma unroll
-            for (int k = 0; k < QK; ++k) {
-                const f32x4 w0 = *(const f32x4 *)&sc.into[32 * k + 8 * g], w1 = *(const f32x4 *)&sc.into[32 * k + 8 * g + 4];
-                f32x8 x = __builtin_convertvector(fx[k][NP - 1], f32x8);
-#pragma unroll
-                for (int q = NP - 2; q >= 0; --q) x += __builtin_convertvector(fx[k][q], f32x8);
-                split(x * __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7), fw[k]);
-            }
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                h[i] *= keep;
-#pragma unroll
-                for (int k = 0; k < QK; ++k) {
-                    bf16x8 fb[NP];
-#pragma unroll
-                    for (int q = 0; q < NP; ++q) fb[q] = *(const bf16x8 *)&sm.bt[q][(16 * i + col) * kS + 32 * k + 8 * g];
-                    h[i] = mma_parts<3>(fb, fw[k], h[i]);
+                    out.template store<WIDE>(yrows, (col * ys + p4 * e | out4) + 16 * i * ys, P - p4);
                 }
             }
             __syncthreads();
