@@ -302,18 +302,16 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
             }
         };
         // One wave forms a chunk's scalars, its lanes the tokens, while the others are at the chunk before.
-        float rdt = 0.0f;
+        Piece<T, 1> rdt;         // (converted where it is used, so that nothing waits for it before)
         auto fetch_dt = [&](int chunk) {
             const int t0 = chunk * Q;
-            Piece<T, 1> d;
             const uint32_t ds = (uint32_t)a.dt_stride * e;
-            d.template load<false>(rows_at(dtp + (int64_t)t0 * a.dt_stride, min(length - t0, Q), ds), lane * ds, 1);
-            rdt = (float)d.v[0];
+            rdt.template load<false>(rows_at(dtp + (int64_t)t0 * a.dt_stride, min(length - t0, Q), ds), lane * ds, 1);
         };
         auto scalars = [&](int chunk) {
             Scalars &sc = sm.sc[chunk & (kSc - 1)];
             const bool live = lane < Q && chunk * Q + lane < length;
-            float delta = rdt + dt_bias;
+            float delta = (float)rdt.v[0] + dt_bias;
             if (a.softplus) delta = softplus_fast(delta);
             if (!live) delta = 0.0f;
             double s = (double)delta * rate * 1.4426950408889634;
