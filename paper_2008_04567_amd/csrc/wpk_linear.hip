@@ -1,4 +1,12 @@
 // Matrix product y = act(x w^T + bias) + residual.
+//
+// Three kernels share the work.  All of them multiply with w's rows as the MFMA's rows and x's as its columns, so a lane holds
+// four neighbouring columns of one row of y at a time.
+//   rows    few rows of x (a token of every request): w is streamed once, straight into registers, the reduction dealt out
+//           to the waves of a workgroup (bound: w's bytes)
+//   tiles   more rows: tiles of x and w through LDS (bound: the matrix pipes)
+//   join    sums the partial products of workgroups that share an output along the reduction, in a fixed order
+// fp32 is multiplied as such by the first, and as sums of three bf16 numbers by the second.
 #include "wpk_seq.h"
 
 namespace wpk {
@@ -6,48 +14,380 @@ namespace wpk {
 struct LinearArgs {
     const void *x, *w, *bias, *residual;
     void *y;
+    float *part;                      // partial products [slice][m][part_stride], where the reduction is cut
     int32_t m, n, k, act, y_f32;
-    int64_t x_stride, w_stride, y_stride, residual_stride;
+    int32_t slices, slice_k;          // reduction entries of a slice (a multiple of 64)
+    int32_t wide_y;                   // rows of y (and the residual, the bias) hold whole aligned groups of four
+    int64_t x_stride, w_stride, y_stride, residual_stride, part_stride;
 };
 
-// 64 x 64 outputs a workgroup, 4 x 4 a lane, operands through LDS 16 of the reduction at a time, fp32 multiply-adds.
-template <typename T> __global__ void __launch_bounds__(256) linear_plain_kernel(LinearArgs a)
+template <typename T> struct Mma;
+template <> struct Mma<bf16> {
+    typedef bf16x8 v8;
+    static __device__ f32x4 m16(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ f32x16 m32(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mma<f16> {
+    typedef f16x8 v8;
+    static __device__ f32x4 m16(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ f32x16 m32(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mma<float> {
+    typedef f32x8 v8;
+    // (the order of the reduction's entries does not matter as long as both operands have it: lane group g gives entry 8 g + j
+    // to the j-th of eight steps of four)
+    static __device__ f32x4 m16(v8 a, v8 b, f32x4 c)
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// eight neighbouring elements from an address that is aligned to one of them (the device takes such loads)
+template <typename T> struct Octet {
+    typedef T vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    static __device__ typename Mma<T>::v8 load(const T *p) { return *(const vec *)p; }
+    static __device__ typename Mma<T>::v8 load_some(const T *p, int left)
+    {
+        typename Mma<T>::v8 v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (T)0.0f;
+        return v;
+    }
+};
+
+// What follows the sums: columns n .. n + 3 of row m.
+template <typename T, typename Y> __device__ inline void finish(const LinearArgs &a, int m, int n, f32x4 v)
 {
-    __shared__ float xs[16][65], ws[16][65];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
-    const T *x = (const T *)a.x, *w = (const T *)a.w;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < a.k; k0 += 16) {
+    typedef T tvec __attribute__((ext_vector_type(4)));
+    typedef Y yvec __attribute__((ext_vector_type(4)));
+    if (m >= a.m || n >= a.n) return;
+    Y *const y = (Y *)a.y + (int64_t)m * a.y_stride + n;
+    const T *const r = (const T *)a.residual + (int64_t)m * a.residual_stride + n, *const b = (const T *)a.bias + n;
+    if (a.wide_y) {
+        if (a.bias) v += __builtin_convertvector(*(const tvec *)b, f32x4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = apply_act<Y>(v[i], a.act);
+        if (a.residual) v += __builtin_convertvector(*(const tvec *)r, f32x4);
+        *(yvec *)y = __builtin_convertvector(v, yvec);
+    } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int row = ty + 16 * i, kk = k0 + tx;
-            xs[tx][row] = m0 + row < a.m && kk < a.k ? (float)x[(int64_t)(m0 + row) * a.x_stride + kk] : 0.0f;
-            ws[tx][row] = n0 + row < a.n && kk < a.k ? (float)w[(int64_t)(n0 + row) * a.w_stride + kk] : 0.0f;
+            if (n + i >= a.n) break;
+            float s = v[i];
+            if (a.bias) s += (float)b[i];
+            s = apply_act<Y>(s, a.act);
+            if (a.residual) s += (float)r[i];
+            y[i] = (Y)s;
         }
-        __syncthreads();
+    }
+}
+template <typename T> __device__ inline void finish(const LinearArgs &a, int m, int n, f32x4 v)
+{
+    if (sizeof(T) == 4 || a.y_f32) finish<T, float>(a, m, n, v);
+    else finish<T, T>(a, m, n, v);
+}
+// ... or, where the reduction is cut, the partial sums
+template <typename T> __device__ inline void finish_or_part(const LinearArgs &a, int slice, int m, int n, f32x4 v)
+{
+    if (a.slices == 1) finish<T>(a, m, n, v);
+    else if (m < a.m && n < a.n) *(f32x4 *)(a.part + ((int64_t)slice * a.m + m) * a.part_stride + n) = v;
+}
+
+template <typename T> __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs a)
+{
+    const int quads = (a.n + 3) / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)quads * a.m) return;
+    const int m = (int)(i / quads), n = (int)(i - (int64_t)m * quads) * 4;
+    f32x4 v = {0, 0, 0, 0};
+    for (int s = 0; s < a.slices; ++s) v += *(const f32x4 *)(a.part + ((int64_t)s * a.m + m) * a.part_stride + n);
+    finish<T>(a, m, n, v);
+}
+
+// ---- few rows ------------------------------------------------------------------------------------------------
+// A workgroup of eight waves owns 16 NT columns of y and all of up to 16 MT rows.  A wave takes every eighth run of 64
+// reduction entries (a line of a row of w in 16-bit types) of its slice and keeps U of them in flight.  Rows beyond the
+// matrices are read as the last one; nothing of them is stored.
+static const int kRowsWaves = 8;
+template <typename T, int MT, int NT, int U> __global__ void __launch_bounds__(64 * kRowsWaves) linear_rows_kernel(LinearArgs a)
+{
+    typedef typename Mma<T>::v8 v8;
+    __shared__ __align__(16) f32x4 sums[kRowsWaves][MT * NT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 16 * NT, slice = blockIdx.y;
+    const int k_end = min(a.k, (slice + 1) * a.slice_k), k_begin = slice * a.slice_k + 64 * wave;
+    const T *wp[NT], *xp[MT];
 #pragma unroll
-        for (int k = 0; k < 16; ++k)
+    for (int i = 0; i < NT; ++i) wp[i] = (const T *)a.w + (int64_t)min(n0 + 16 * i + row, a.n - 1) * a.w_stride + 8 * g;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < MT; ++i) xp[i] = (const T *)a.x + (int64_t)min(16 * i + row, a.m - 1) * a.x_stride + 8 * g;
+    f32x4 acc[MT][NT];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(xs[k][ty + 16 * i], ws[k][tx + 16 * j], acc[i][j]);
-        __syncthreads();
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+
+    v8 fw[U][2][NT], fx[U][2][MT];
+    auto fetch = [&](int u, int k) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i) fw[u][h][i] = Octet<T>::load(wp[i] + k + 32 * h);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) fx[u][h][i] = Octet<T>::load(xp[i] + k + 32 * h);
+        }
+    };
+    auto multiply = [&](int u) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = Mma<T>::m16(fw[u][h][j], fx[u][h][i], acc[i][j]);
+    };
+    const int step = 64 * kRowsWaves;
+    int k = k_begin;
+    // U runs in flight: run u is asked for again as soon as it has been multiplied
+    if (k + (U - 1) * step + 64 <= k_end) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) fetch(u, k + u * step);
+        for (; k + (2 * U - 1) * step + 64 <= k_end; k += U * step) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                multiply(u);
+                fetch(u, k + (U + u) * step);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) multiply(u);
+        k += U * step;
+    }
+    for (; k + 64 <= k_end; k += step) {
+        fetch(0, k);
+        multiply(0);
+    }
+    if (k < k_end) {                  // the reduction's last entries, fewer than 64
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int left = k_end - (k + 32 * h + 8 * g);
+#pragma unroll
+            for (int i = 0; i < NT; ++i) fw[0][h][i] = Octet<T>::load_some(wp[i] + k + 32 * h, left);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) fx[0][h][i] = Octet<T>::load_some(xp[i] + k + 32 * h, left);
+        }
+        multiply(0);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-            if (m >= a.m || n >= a.n) continue;
-            float v = acc[i][j];
-            if (a.bias) v += (float)((const T *)a.bias)[n];
-            v = a.y_f32 ? apply_act<float>(v, a.act) : apply_act<T>(v, a.act);
-            if (a.residual) v += (float)((const T *)a.residual)[(int64_t)m * a.residual_stride + n];
-            if (a.y_f32) ((float *)a.y)[(int64_t)m * a.y_stride + n] = v;
-            else ((T *)a.y)[(int64_t)m * a.y_stride + n] = (T)v;
-        }
+        for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int t = wave; t < MT * NT; t += kRowsWaves) {
+        f32x4 v = sums[0][t][lane];
+#pragma unroll
+        for (int s = 1; s < kRowsWaves; ++s) v += sums[s][t][lane];
+        finish_or_part<T>(a, slice, 16 * (t / NT) + row, n0 + 16 * (t % NT) + 4 * g, v);
+    }
 }
+
+// ---- tiles -----------------------------------------------------------------------------------------------------
+// Workgroups are dealt out to the eight dies in turn: give each a run of tiles that share rows of x and w in its cache.
+struct TileAt {
+    int m, n;
+};
+__device__ inline TileAt tile_of(int id, int tiles_m, int tiles_n)
+{
+    const int all = tiles_m * tiles_n, each = all / kNumXcd, more = all % kNumXcd, die = id % kNumXcd;
+    const int t = die * each + min(die, more) + id / kNumXcd;
+    const int kBand = 8;              // tiles of a band of rows go down its columns
+    const int band = t / (kBand * tiles_n), rows = min(kBand, tiles_m - band * kBand), in = t - band * kBand * tiles_n;
+    return {band * kBand + in % rows, in / rows};
+}
+
+template <typename T> struct TileType {
+    typedef T part_t;
+    static const int parts = 1, bk = 64;
+};
+template <> struct TileType<float> {
+    typedef bf16 part_t;
+    static const int parts = 3, bk = 32;
+};
+
+// fp32 operands are scaled by 2^16 before they are cut into three bf16 numbers, so that the smallest numbers' parts are
+// numbers still; what overflows by that shows in the sums, and is summed again as it stands.
+static const float kSplitScale = 65536.0f;
+
+// BM rows of y (columns of the MFMA) by BN columns, WM x WN waves of 32 x 32 blocks.  Operands of the step after the next
+// ... are held in registers while a step's are multiplied, and stored to the other LDS buffer.
+template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN) linear_tiles_kernel(LinearArgs a)
+{
+    typedef typename TileType<T>::part_t part_t;
+    typedef typename Mma<part_t>::v8 p8;
+    const int NP = TileType<T>::parts, BK = TileType<T>::bk, kRow = BK + 8, kThreads = 64 * WM * WN;
+    const int TM = BM / WM / 32, TN = BN / WN / 32, kOctets = BK / 8, kPer = (BM + BN) * kOctets / kThreads;
+    static_assert((BM + BN) * kOctets % kThreads == 0 && BN * kOctets % kThreads == 0, "whole rounds of loads");
+    __shared__ __align__(16) part_t lds[2][NP][(BM + BN) * kRow];      // rows of w, then rows of x
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 31, half = lane >> 5;
+    const int wm = wave % WM, wn = wave / WM, slice = blockIdx.y;
+    const TileAt at = tile_of(blockIdx.x, (a.m + BM - 1) / BM, (a.n + BN - 1) / BN);
+    const int m0 = at.m * BM, n0 = at.n * BN;
+    const int k_begin = slice * a.slice_k, k_end = min(a.k, k_begin + a.slice_k);
+
+    const T *src[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int task = tid + i * kThreads, r = task / kOctets, o = task % kOctets;
+        src[i] = r < BN ? (const T *)a.w + (int64_t)min(n0 + r, a.n - 1) * a.w_stride + 8 * o
+                        : (const T *)a.x + (int64_t)min(m0 + r - BN, a.m - 1) * a.x_stride + 8 * o;
+    }
+    typename Mma<T>::v8 held[kPer];
+    auto fetch = [&](int k) {
+        if (k + BK <= k_end) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) held[i] = Octet<T>::load(src[i] + k);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) held[i] = Octet<T>::load_some(src[i] + k, k_end - k - (tid + i * kThreads) % kOctets * 8);
+        }
+    };
+    auto stage = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int task = tid + i * kThreads, to = task / kOctets * kRow + task % kOctets * 8;
+            if constexpr (NP == 1) {
+                *(p8 *)&lds[buf][0][to] = held[i];
+            } else {
+                f32x8 v = held[i] * kSplitScale;
+#pragma unroll
+                for (int q = 0; q < NP; ++q) {
+                    const p8 u = __builtin_convertvector(v, p8);
+                    v -= __builtin_convertvector(u, f32x8);
+                    *(p8 *)&lds[buf][q][to] = u;
+                }
+            }
+        }
+    };
+    f32x16 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+    fetch(k_begin);
+    stage(0);
+    __syncthreads();
+    int buf = 0;
+    for (int k = k_begin; k < k_end; k += BK, buf ^= 1) {
+        const bool more = k + BK < k_end;
+        if (more) fetch(k + BK);
+#pragma unroll
+        for (int s = 0; s < BK / 16; ++s) {
+            p8 fw[TN][NP], fx[TM][NP];
+#pragma unroll
+            for (int q = 0; q < NP; ++q) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) fw[j][q] = *(const p8 *)&lds[buf][q][(wn * TN * 32 + j * 32 + row) * kRow + 16 * s + 8 * half];
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fx[i][q] = *(const p8 *)&lds[buf][q][(BN + wm * TM * 32 + i * 32 + row) * kRow + 16 * s + 8 * half];
+            }
+#pragma unroll
+            for (int u = 0; u < NP; ++u)
+#pragma unroll
+                for (int v = 0; u + v < NP; ++v)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) acc[i][j] = Mma<part_t>::m32(fw[j][u], fx[i][v], acc[i][j]);
+        }
+        if (more) stage(buf ^ 1);
+        __syncthreads();
+    }
+
+    float scale = 1.0f;
+    bool odd = false;                 // infinities, NaN, or numbers that the scaled parts could not hold
+    if constexpr (NP > 1) {
+        scale = 1.0f / (kSplitScale * kSplitScale);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) odd = odd || !(fabsf(acc[i][j][r]) <= 3.4028234e38f);
+        odd = __any(odd);
+    }
+    // Through LDS, 32 rows a wave at a time, so that y is written (and the residual read) in whole lines and what follows
+    // the sums stands in the code once.
+    const int kCols = 32 * TN, kPitch = kCols + 4, kQuads = kCols / 4;
+    static_assert(sizeof(lds) >= sizeof(float) * WM * WN * 32 * kPitch, "the waves' rows fit");
+    float *const rows = (float *)&lds[0][0][0] + wave * 32 * kPitch;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *(f32x4 *)&rows[row * kPitch + 32 * j + 2 * r + 4 * half] =
+                    f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
+#pragma unroll 1
+        for (int t = lane; t < 32 * kQuads; t += 64) {
+            const int m = m0 + (wm * TM + i) * 32 + t / kQuads, n = n0 + wn * kCols + t % kQuads * 4;
+            f32x4 v = *(const f32x4 *)&rows[t / kQuads * kPitch + t % kQuads * 4] * scale;
+            if (NP > 1 && odd) {
+                const T *const xr = (const T *)a.x + (int64_t)min(m, a.m - 1) * a.x_stride;
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    const T *const wr = (const T *)a.w + (int64_t)min(n + c, a.n - 1) * a.w_stride;
+                    float sum = 0.0f;
+#pragma unroll 1
+                    for (int k = k_begin; k < k_end; ++k) sum = fmaf((float)xr[k], (float)wr[k], sum);
+                    v[0] = c == 0 ? sum : v[0];
+                    v[1] = c == 1 ? sum : v[1];
+                    v[2] = c == 2 ? sum : v[2];
+                    v[3] = c == 3 ? sum : v[3];
+                }
+            }
+            finish_or_part<T>(a, slice, m, n, v);
+        }
+    }
+}
+
+// ---- which of them ------------------------------------------------------------------------------------------------
+static const int kRowsMost = 64;      // rows of x that the row kernel takes
+struct LinearShape {
+    int tile;                         // 0: the row kernel
+    int slices, slice_k;
+};
+
+static LinearShape linear_shape(const wpk_linear_desc &d)
+{
+    LinearShape s = {0, 1, (d.k + 63) / 64 * 64};
+    const int64_t steps = (d.k + 63) / 64;
+    int64_t groups, slices;
+    if (d.m <= kRowsMost) {
+        groups = (d.n + 15) / 16;
+        // each of the eight waves keeps four runs of 64 at least
+        slices = kComputeUnits / groups;
+        if (slices > steps / (4 * kRowsWaves)) slices = steps / (4 * kRowsWaves);
+    } else {
+        s.tile = 128;
+        auto tiles = [&](int t) { return (int64_t)((d.m + t - 1) / t) * ((d.n + t - 1) / t); };
+        if (tiles(128) < kComputeUnits / 2) s.tile = 64;
+        groups = tiles(s.tile);
+        slices = kComputeUnits / groups;
+        if (slices > steps / 8) slices = steps / 8;
+    }
+    if (slices > 16) slices = 16;
+    if (slices < 2) return s;
+    s.slice_k = (int)((steps + slices - 1) / slices) * 64;
+    s.slices = (d.k + s.slice_k - 1) / s.slice_k;
+    return s;
+}
+
+static int64_t part_stride(const wpk_linear_desc &d) { return ((int64_t)d.n + 3) / 4 * 4; }
 
 static int check_linear(const wpk_linear_desc *dp)
 {
@@ -62,9 +402,34 @@ static int check_linear(const wpk_linear_desc *dp)
     return WPK_OK;
 }
 
-template <typename T> static int linear_typed(const LinearArgs &a, hipStream_t st)
+template <typename T> static int launch_rows(const LinearArgs &a, hipStream_t st)
 {
-    hipLaunchKernelGGL((linear_plain_kernel<T>), dim3((a.n + 63) / 64, (a.m + 63) / 64), dim3(256), 0, st, a);
+    const int kThreads = 64 * kRowsWaves;
+    const dim3 grid((a.n + 15) / 16, a.slices);
+    if (a.m <= 16) hipLaunchKernelGGL((linear_rows_kernel<T, 1, 1, 4>), grid, dim3(kThreads), 0, st, a);
+    else if (a.m <= 32) hipLaunchKernelGGL((linear_rows_kernel<T, 2, 1, 2>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((linear_rows_kernel<T, 4, 1, 1>), grid, dim3(kThreads), 0, st, a);
+    WPK_HIP(hipGetLastError());
+    return WPK_OK;
+}
+
+template <typename T, int B, int W> static int launch_tiles(const LinearArgs &a, hipStream_t st)
+{
+    const dim3 grid((unsigned)(((a.m + B - 1) / B) * ((a.n + B - 1) / B)), a.slices);
+    hipLaunchKernelGGL((linear_tiles_kernel<T, B, B, W, W>), grid, dim3(64 * W * W), 0, st, a);
+    WPK_HIP(hipGetLastError());
+    return WPK_OK;
+}
+
+template <typename T> static int linear_typed(const LinearArgs &a, const LinearShape &s, hipStream_t st)
+{
+    int rc;
+    if (s.tile == 0) rc = launch_rows<T>(a, st);
+    else if (s.tile == 64) rc = launch_tiles<T, 64, 2>(a, st);
+    else rc = launch_tiles<T, 128, 2>(a, st);
+    if (rc != WPK_OK || a.slices == 1) return rc;
+    const int64_t quads = (int64_t)((a.n + 3) / 4) * a.m;
+    hipLaunchKernelGGL((linear_join_kernel<T>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a);
     WPK_HIP(hipGetLastError());
     return WPK_OK;
 }
@@ -76,7 +441,9 @@ extern "C" {
 int64_t wpk_linear_workspace_bytes(const wpk_linear_desc *d)
 {
     const int rc = wpk::check_linear(d);
-    return rc == WPK_OK ? 0 : rc;
+    if (rc != WPK_OK) return rc;
+    const wpk::LinearShape s = wpk::linear_shape(*d);
+    return s.slices < 2 ? 0 : (int64_t)s.slices * d->m * wpk::part_stride(*d) * (int64_t)sizeof(float);
 }
 
 int wpk_linear_fwd(const wpk_linear_desc *dp, const void *x, const void *w, const void *bias, const void *residual, void *y,
@@ -88,16 +455,20 @@ int wpk_linear_fwd(const wpk_linear_desc *dp, const void *x, const void *w, cons
     const wpk_linear_desc d = *dp;
     if (d.m == 0) return WPK_OK;
     if (!x || !w || !y) return WPK_E_NULL_PTR;
-    const size_t e = seq_type_bytes(d.dtype);
-    if (!aligned_to(x, e) || !aligned_to(w, e) || !aligned_to(bias, e) || !aligned_to(residual, e) ||
-        !aligned_to(y, seq_type_bytes(d.y_dtype)))
+    const size_t e = seq_type_bytes(d.dtype), ye = seq_type_bytes(d.y_dtype);
+    if (!aligned_to(x, e) || !aligned_to(w, e) || !aligned_to(bias, e) || !aligned_to(residual, e) || !aligned_to(y, ye))
         return WPK_E_BAD_ARG;
-    LinearArgs a = {x, w, bias, residual, y, d.m, d.n, d.k, d.act, d.y_dtype == WPK_F32, d.x_stride, d.w_stride,
-                    d.y_stride, d.residual_stride};
+    const LinearShape s = linear_shape(d);
+    if (s.slices > 1 && !workspace) return WPK_E_NULL_PTR;
+    if (!aligned_to(workspace, 16)) return WPK_E_BAD_ARG;
+    const bool wide = d.n % 4 == 0 && d.y_stride % 4 == 0 && aligned_to(y, 4 * ye) && aligned_to(bias, 4 * e) &&
+                      (!residual || (d.residual_stride % 4 == 0 && aligned_to(residual, 4 * e)));
+    LinearArgs a = {x, w, bias, residual, y, (float *)workspace, d.m, d.n, d.k, d.act, d.y_dtype == WPK_F32,
+                    s.slices, s.slice_k, wide, d.x_stride, d.w_stride, d.y_stride, d.residual_stride, part_stride(d)};
     const hipStream_t st = (hipStream_t)stream;
-    if (d.dtype == WPK_BF16) return linear_typed<bf16>(a, st);
-    if (d.dtype == WPK_F16) return linear_typed<f16>(a, st);
-    return linear_typed<float>(a, st);
+    if (d.dtype == WPK_BF16) return linear_typed<bf16>(a, s, st);
+    if (d.dtype == WPK_F16) return linear_typed<f16>(a, s, st);
+    return linear_typed<float>(a, s, st);
 }
 
 }  // extern "C"
