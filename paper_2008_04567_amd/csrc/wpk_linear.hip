@@ -219,6 +219,45 @@ template <> struct TileType<float> {
 // numbers still; what overflows by that shows in the sums, and is summed again as it stands.
 static const float kSplitScale = 65536.0f;
 
+// A wave's blocks go to y through LDS, 32 rows at a time, so that y is written (and the residual read) in whole lines and what
+// follows the sums stands in the code once.  `odd`: the sums are not to be used, they are formed again one by one in fp32.
+template <typename T, int TM, int TN>
+__device__ inline void put_tile(const LinearArgs &a, const f32x16 (&acc)[TM][TN], float *rows, float scale, bool odd, int slice,
+                                int k_begin, int k_end, int m0, int n0)
+{
+    const int kCols = 32 * TN, kPitch = kCols + 4, kQuads = kCols / 4;
+    const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *(f32x4 *)&rows[row * kPitch + 32 * j + 2 * r + 4 * half] =
+                    f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
+#pragma unroll 1
+        for (int t = lane; t < 32 * kQuads; t += 64) {
+            const int m = m0 + i * 32 + t / kQuads, n = n0 + t % kQuads * 4;
+            f32x4 v = *(const f32x4 *)&rows[t / kQuads * kPitch + t % kQuads * 4] * scale;
+            if (sizeof(T) == 4 && odd) {
+                const T *const xr = (const T *)a.x + (int64_t)min(m, a.m - 1) * a.x_stride;
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    const T *const wr = (const T *)a.w + (int64_t)min(n + c, a.n - 1) * a.w_stride;
+                    float sum = 0.0f;
+#pragma unroll 1
+                    for (int k = k_begin; k < k_end; ++k) sum = fmaf((float)xr[k], (float)wr[k], sum);
+                    v[0] = c == 0 ? sum : v[0];
+                    v[1] = c == 1 ? sum : v[1];
+                    v[2] = c == 2 ? sum : v[2];
+                    v[3] = c == 3 ? sum : v[3];
+                }
+            }
+            finish_or_part<T>(a, slice, m, n, v);
+        }
+    }
+}
+
 // BM rows of y (columns of the MFMA) by BN columns, WM x WN waves of 32 x 32 blocks.  Operands of the step after the next
 // ... are held in registers while a step's are multiplied, and stored to the other LDS buffer.
 template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN) linear_tiles_kernel(LinearArgs a)
@@ -229,6 +268,7 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
     const int TM = BM / WM / 32, TN = BN / WN / 32, kOctets = BK / 8, kPer = (BM + BN) * kOctets / kThreads;
     static_assert((BM + BN) * kOctets % kThreads == 0 && BN * kOctets % kThreads == 0, "whole rounds of loads");
     __shared__ __align__(16) part_t lds[2][NP][(BM + BN) * kRow];      // rows of w, then rows of x
+    static_assert(sizeof(lds) >= sizeof(float) * WM * WN * 32 * (32 * TN + 4), "what put_tile needs");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 31, half = lane >> 5;
     const int wm = wave % WM, wn = wave / WM, slice = blockIdx.y;
     const TileAt at = tile_of(blockIdx.x, (a.m + BM - 1) / BM, (a.n + BN - 1) / BN);
@@ -319,46 +359,89 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
                 for (int r = 0; r < 16; ++r) odd = odd || !(fabsf(acc[i][j][r]) <= 3.4028234e38f);
         odd = __any(odd);
     }
-    // Through LDS, 32 rows a wave at a time, so that y is written (and the residual read) in whole lines and what follows
-    // the sums stands in the code once.
-    const int kCols = 32 * TN, kPitch = kCols + 4, kQuads = kCols / 4;
-    static_assert(sizeof(lds) >= sizeof(float) * WM * WN * 32 * kPitch, "the waves' rows fit");
-    float *const rows = (float *)&lds[0][0][0] + wave * 32 * kPitch;
+    put_tile<T, TM, TN>(a, acc, (float *)&lds[0][0][0] + wave * 32 * (32 * TN + 4), scale, odd, slice, k_begin, k_end,
+                        m0 + wm * TM * 32, n0 + wn * TN * 32);
+}
+
+// The same for 16-bit operands in aligned rows: loads write LDS directly, a step ahead, and take no registers.  A wave's load
+// brings eight rows of 64 entries; the 16-byte pieces of row r stand in the order of their number xor r mod 8, which the lanes
+// bring about by what they ask for, so that reading the same piece of eight rows takes all banks.
+template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN, 2)
+linear_direct_kernel(LinearArgs a)
+{
+    typedef typename Mma<T>::v8 v8;
+    const int BK = 64, kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, kLoads = (BM + BN) / 8 / kWaves;
+    static_assert(BN / 8 % kLoads == 0, "a wave loads rows of one matrix");
+    __shared__ __align__(16) T lds[2][(BM + BN) * BK];         // rows of w, then rows of x
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 31, half = lane >> 5;
+    const int wm = wave % WM, wn = wave / WM, slice = blockIdx.y;
+    const TileAt at = tile_of(blockIdx.x, (a.m + BM - 1) / BM, (a.n + BN - 1) / BN);
+    const int m0 = at.m * BM, n0 = at.n * BN;
+    const int k_begin = slice * a.slice_k, k_end = min(a.k, k_begin + a.slice_k);
+
+    const bool of_w = wave * kLoads < BN / 8;
+    const int r0 = (of_w ? n0 : m0) + (wave * kLoads - (of_w ? 0 : BN / 8)) * 8, last = (of_w ? a.n : a.m) - 1;
+    const int64_t stride = of_w ? a.w_stride : a.x_stride;
+    const int base = min(r0, last), piece = ((lane & 7) ^ (lane >> 3)) * 8;
+    const Rows src = __builtin_amdgcn_make_buffer_rsrc((T *)(of_w ? a.w : a.x) + base * stride, 0, 0x7fffffff, 0x00020000);
+    uint32_t from[kLoads];                                     // rows beyond the matrix are read as its last one
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
+    for (int i = 0; i < kLoads; ++i) from[i] = (uint32_t)((min(r0 + 8 * i + (lane >> 3), last) - base) * (int)stride + piece) * sizeof(T);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)&lds[0][0] + wave * kLoads * 8 * BK * sizeof(T);
+    auto fetch = [&](int buf, int k) {
+        const uint32_t to = lds0 + buf * (uint32_t)sizeof(lds[0]);
+        const bool whole = k + BK <= k_end;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const uint32_t off = whole || k + piece < k_end ? from[i] : kOutside;      // (outside: zeros)
+            asm volatile("s_mov_b32 m0, %2\n s_nop 0\n buffer_load_dwordx4 %0, %1, %3 offen lds"
+                         :
+                         : "v"(off), "s"(src), "s"(to + i * 8 * BK * (uint32_t)sizeof(T)), "s"(k * (uint32_t)sizeof(T))
+                         : "memory");
+        }
+    };
+    uint32_t read[4];                                          // where this lane's piece of a block's 16 entries is
+#pragma unroll
+    for (int s = 0; s < 4; ++s) read[s] = row * BK + (((2 * s + half) ^ (lane & 7)) * 8);
+
+    f32x16 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                *(f32x4 *)&rows[row * kPitch + 32 * j + 2 * r + 4 * half] =
-                    f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
-#pragma unroll 1
-        for (int t = lane; t < 32 * kQuads; t += 64) {
-            const int m = m0 + (wm * TM + i) * 32 + t / kQuads, n = n0 + wn * kCols + t % kQuads * 4;
-            f32x4 v = *(const f32x4 *)&rows[t / kQuads * kPitch + t % kQuads * 4] * scale;
-            if (NP > 1 && odd) {
-                const T *const xr = (const T *)a.x + (int64_t)min(m, a.m - 1) * a.x_stride;
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    const T *const wr = (const T *)a.w + (int64_t)min(n + c, a.n - 1) * a.w_stride;
-                    float sum = 0.0f;
-#pragma unroll 1
-                    for (int k = k_begin; k < k_end; ++k) sum = fmaf((float)xr[k], (float)wr[k], sum);
-                    v[0] = c == 0 ? sum : v[0];
-                    v[1] = c == 1 ? sum : v[1];
-                    v[2] = c == 2 ? sum : v[2];
-                    v[3] = c == 3 ? sum : v[3];
-                }
-            }
-            finish_or_part<T>(a, slice, m, n, v);
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+    fetch(0, k_begin);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    int buf = 0;
+    for (int k = k_begin; k < k_end; k += BK, buf ^= 1) {
+        if (k + BK < k_end) fetch(buf ^ 1, k + BK);
+        const T *const pw = &lds[buf][wn * TN * 32 * BK], *const px = &lds[buf][(BN + wm * TM * 32) * BK];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            v8 fw[TN], fx[TM];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fw[j] = *(const v8 *)(pw + read[s] + j * 32 * BK);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fx[i] = *(const v8 *)(px + read[s] + i * 32 * BK);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = Mma<T>::m32(fw[j], fx[i], acc[i][j]);
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
     }
+    put_tile<T, TM, TN>(a, acc, (float *)&lds[0][0] + wave * 32 * (32 * TN + 4), 1.0f, false, slice, k_begin, k_end,
+                        m0 + wm * TM * 32, n0 + wn * TN * 32);
 }
 
 // ---- which of them ------------------------------------------------------------------------------------------------
 static const int kRowsMost = 64;      // rows of x that the row kernel takes
 struct LinearShape {
-    int tile;                         // 0: the row kernel
+    int tile;                         // rows and columns of a tile; 0: the row kernel
     int slices, slice_k;
 };
 
@@ -373,9 +456,8 @@ static LinearShape linear_shape(const wpk_linear_desc &d)
         slices = kComputeUnits / groups;
         if (slices > steps / (4 * kRowsWaves)) slices = steps / (4 * kRowsWaves);
     } else {
-        s.tile = 128;
         auto tiles = [&](int t) { return (int64_t)((d.m + t - 1) / t) * ((d.n + t - 1) / t); };
-        if (tiles(128) < kComputeUnits / 2) s.tile = 64;
+        s.tile = d.dtype != WPK_F32 && tiles(256) >= kComputeUnits ? 256 : tiles(128) >= kComputeUnits / 2 ? 128 : 64;
         groups = tiles(s.tile);
         slices = kComputeUnits / groups;
         if (slices > steps / 8) slices = steps / 8;
@@ -413,20 +495,29 @@ template <typename T> static int launch_rows(const LinearArgs &a, hipStream_t st
     return WPK_OK;
 }
 
-template <typename T, int B, int W> static int launch_tiles(const LinearArgs &a, hipStream_t st)
+static unsigned tile_count(const LinearArgs &a, int b) { return (unsigned)(((a.m + b - 1) / b) * ((a.n + b - 1) / b)); }
+
+template <typename T> static int launch_tiles(const LinearArgs &a, int tile, bool direct, hipStream_t st)
 {
-    const dim3 grid((unsigned)(((a.m + B - 1) / B) * ((a.n + B - 1) / B)), a.slices);
-    hipLaunchKernelGGL((linear_tiles_kernel<T, B, B, W, W>), grid, dim3(64 * W * W), 0, st, a);
+    const dim3 grid(tile_count(a, tile), a.slices);
+    if constexpr (sizeof(T) == 2) {
+        if (direct) {
+            if (tile == 256) hipLaunchKernelGGL((linear_direct_kernel<T, 256, 256, 2, 4>), grid, dim3(512), 0, st, a);
+            else if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<T, 128, 128, 2, 2>), grid, dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((linear_direct_kernel<T, 64, 64, 2, 2>), grid, dim3(256), 0, st, a);
+            WPK_HIP(hipGetLastError());
+            return WPK_OK;
+        }
+    }
+    if (tile == 64) hipLaunchKernelGGL((linear_tiles_kernel<T, 64, 64, 2, 2>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((linear_tiles_kernel<T, 128, 128, 2, 2>), dim3(tile_count(a, 128), a.slices), dim3(256), 0, st, a);
     WPK_HIP(hipGetLastError());
     return WPK_OK;
 }
 
-template <typename T> static int linear_typed(const LinearArgs &a, const LinearShape &s, hipStream_t st)
+template <typename T> static int linear_typed(const LinearArgs &a, const LinearShape &s, bool direct, hipStream_t st)
 {
-    int rc;
-    if (s.tile == 0) rc = launch_rows<T>(a, st);
-    else if (s.tile == 64) rc = launch_tiles<T, 64, 2>(a, st);
-    else rc = launch_tiles<T, 128, 2>(a, st);
+    const int rc = s.tile == 0 ? launch_rows<T>(a, st) : launch_tiles<T>(a, s.tile, direct, st);
     if (rc != WPK_OK || a.slices == 1) return rc;
     const int64_t quads = (int64_t)((a.n + 3) / 4) * a.m;
     hipLaunchKernelGGL((linear_join_kernel<T>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a);
@@ -465,10 +556,12 @@ int wpk_linear_fwd(const wpk_linear_desc *dp, const void *x, const void *w, cons
                       (!residual || (d.residual_stride % 4 == 0 && aligned_to(residual, 4 * e)));
     LinearArgs a = {x, w, bias, residual, y, (float *)workspace, d.m, d.n, d.k, d.act, d.y_dtype == WPK_F32,
                     s.slices, s.slice_k, wide, d.x_stride, d.w_stride, d.y_stride, d.residual_stride, part_stride(d)};
+    // (loads that write LDS move 16 aligned bytes)
+    const bool direct = d.k % 8 == 0 && d.x_stride % 8 == 0 && d.w_stride % 8 == 0 && aligned_to(x, 16) && aligned_to(w, 16);
     const hipStream_t st = (hipStream_t)stream;
-    if (d.dtype == WPK_BF16) return linear_typed<bf16>(a, s, st);
-    if (d.dtype == WPK_F16) return linear_typed<f16>(a, s, st);
-    return linear_typed<float>(a, s, st);
+    if (d.dtype == WPK_BF16) return linear_typed<bf16>(a, s, direct, st);
+    if (d.dtype == WPK_F16) return linear_typed<f16>(a, s, direct, st);
+    return linear_typed<float>(a, s, direct, st);
 }
 
 }  // extern "C"
