@@ -363,46 +363,52 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
                         m0 + wm * TM * 32, n0 + wn * TN * 32);
 }
 
-// The same for 16-bit operands in aligned rows: loads write LDS directly, a step ahead, and take no registers.  A wave's load
-// brings eight rows of 64 entries; the 16-byte pieces of row r stand in the order of their number xor r mod 8, which the lanes
-// bring about by what they ask for, so that reading the same piece of eight rows takes all banks.
-template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN, 2)
+// The same for 16-bit operands in aligned rows: loads write LDS directly and take no registers, STAGES - 1 steps of BK entries
+// ahead of the products.  A wave's load brings 1024 bytes of whole rows.  The 16-byte pieces of a row stand in the order of their
+// number xor some bits of the row's, which the lanes bring about by what they ask for: the lanes that read the same piece of
+// 32 rows take all banks alike.
+template <typename T, int BM, int BN, int WM, int WN, int BK, int STAGES> __global__ void __launch_bounds__(64 * WM * WN, 2)
 linear_direct_kernel(LinearArgs a)
 {
     typedef typename Mma<T>::v8 v8;
-    const int BK = 64, kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, kLoads = (BM + BN) / 8 / kWaves;
-    static_assert(BN / 8 % kLoads == 0, "a wave loads rows of one matrix");
-    __shared__ __align__(16) T lds[2][(BM + BN) * BK];         // rows of w, then rows of x
+    const int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+    const int kPieces = BK / 8, kLoadRows = 64 / kPieces, kLoads = (BM + BN) / kLoadRows / kWaves;
+    static_assert(BN / kLoadRows % kLoads == 0, "a wave loads rows of one matrix");
+    __shared__ __align__(16) T lds[STAGES][(BM + BN) * BK];    // rows of w, then rows of x
+    static_assert(sizeof(lds) >= sizeof(float) * WM * WN * 32 * (32 * TN + 4), "what put_tile needs");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 31, half = lane >> 5;
     const int wm = wave % WM, wn = wave / WM, slice = blockIdx.y;
     const TileAt at = tile_of(blockIdx.x, (a.m + BM - 1) / BM, (a.n + BN - 1) / BN);
     const int m0 = at.m * BM, n0 = at.n * BN;
     const int k_begin = slice * a.slice_k, k_end = min(a.k, k_begin + a.slice_k);
+    auto order = [](int r) { return BK == 64 ? r & 7 : (r >> 2) & 3; };
 
-    const bool of_w = wave * kLoads < BN / 8;
-    const int r0 = (of_w ? n0 : m0) + (wave * kLoads - (of_w ? 0 : BN / 8)) * 8, last = (of_w ? a.n : a.m) - 1;
+    const int w_loads = BN / kLoadRows, load_row = lane / kPieces;
+    const bool of_w = wave * kLoads < w_loads;
+    const int r0 = (of_w ? n0 : m0) + (wave * kLoads - (of_w ? 0 : w_loads)) * kLoadRows, last = (of_w ? a.n : a.m) - 1;
     const int64_t stride = of_w ? a.w_stride : a.x_stride;
-    const int base = min(r0, last), piece = ((lane & 7) ^ (lane >> 3)) * 8;
+    const int base = min(r0, last), piece = (lane % kPieces ^ order(load_row)) * 8;
     const Rows src = __builtin_amdgcn_make_buffer_rsrc((T *)(of_w ? a.w : a.x) + base * stride, 0, 0x7fffffff, 0x00020000);
     uint32_t from[kLoads];                                     // rows beyond the matrix are read as its last one
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) from[i] = (uint32_t)((min(r0 + 8 * i + (lane >> 3), last) - base) * (int)stride + piece) * sizeof(T);
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)&lds[0][0] + wave * kLoads * 8 * BK * sizeof(T);
-    auto fetch = [&](int buf, int k) {
-        const uint32_t to = lds0 + buf * (uint32_t)sizeof(lds[0]);
+    for (int i = 0; i < kLoads; ++i)
+        from[i] = (uint32_t)((min(r0 + kLoadRows * i + load_row, last) - base) * (int)stride + piece) * sizeof(T);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)&lds[0][0] + wave * kLoads * 1024;
+    auto fetch = [&](int stage, int k) {
+        const uint32_t to = lds0 + stage * (uint32_t)sizeof(lds[0]);
         const bool whole = k + BK <= k_end;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const uint32_t off = whole || k + piece < k_end ? from[i] : kOutside;      // (outside: zeros)
             asm volatile("s_mov_b32 m0, %2\n s_nop 0\n buffer_load_dwordx4 %0, %1, %3 offen lds"
                          :
-                         : "v"(off), "s"(src), "s"(to + i * 8 * BK * (uint32_t)sizeof(T)), "s"(k * (uint32_t)sizeof(T))
+                         : "v"(off), "s"(src), "s"(to + i * 1024), "s"(k * (uint32_t)sizeof(T))
                          : "memory");
         }
     };
-    uint32_t read[4];                                          // where this lane's piece of a block's 16 entries is
+    uint32_t read[BK / 16];                                    // where this lane's piece of a block's 16 entries is
 #pragma unroll
-    for (int s = 0; s < 4; ++s) read[s] = row * BK + (((2 * s + half) ^ (lane & 7)) * 8);
+    for (int s = 0; s < BK / 16; ++s) read[s] = row * BK + ((2 * s + half) ^ order(row)) * 8;
 
     f32x16 acc[TM][TN];
 #pragma unroll
@@ -412,15 +418,18 @@ linear_direct_kernel(LinearArgs a)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-    fetch(0, k_begin);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    int buf = 0;
-    for (int k = k_begin; k < k_end; k += BK, buf ^= 1) {
-        if (k + BK < k_end) fetch(buf ^ 1, k + BK);
-        const T *const pw = &lds[buf][wn * TN * 32 * BK], *const px = &lds[buf][(BN + wm * TM * 32) * BK];
+    // Steps behind the last are asked for as well, all of them outside, so that the same number of loads is always under way.
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+    for (int s = 0; s < STAGES - 1; ++s) fetch(s, k_begin + s * BK);
+    int stage = 0;
+    for (int k = k_begin; k < k_end; k += BK) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * kLoads) : "memory");
+        __builtin_amdgcn_s_barrier();        // this step's operands are there, and nobody reads the last step's any more
+        const int behind = stage == 0 ? STAGES - 1 : stage - 1;
+        fetch(behind, k + (STAGES - 1) * BK);
+        const T *const pw = &lds[stage][wn * TN * 32 * BK], *const px = &lds[stage][(BN + wm * TM * 32) * BK];
+#pragma unroll
+        for (int s = 0; s < BK / 16; ++s) {
             v8 fw[TN], fx[TM];
 #pragma unroll
             for (int j = 0; j < TN; ++j) fw[j] = *(const v8 *)(pw + read[s] + j * 32 * BK);
@@ -431,9 +440,10 @@ linear_direct_kernel(LinearArgs a)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) acc[i][j] = Mma<T>::m32(fw[j], fx[i], acc[i][j]);
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the loads of zeros write LDS too)
+    __syncthreads();
     put_tile<T, TM, TN>(a, acc, (float *)&lds[0][0] + wave * 32 * (32 * TN + 4), 1.0f, false, slice, k_begin, k_end,
                         m0 + wm * TM * 32, n0 + wn * TN * 32);
 }
@@ -502,9 +512,9 @@ template <typename T> static int launch_tiles(const LinearArgs &a, int tile, boo
     const dim3 grid(tile_count(a, tile), a.slices);
     if constexpr (sizeof(T) == 2) {
         if (direct) {
-            if (tile == 256) hipLaunchKernelGGL((linear_direct_kernel<T, 256, 256, 2, 4>), grid, dim3(512), 0, st, a);
-            else if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<T, 128, 128, 2, 2>), grid, dim3(256), 0, st, a);
-            else hipLaunchKernelGGL((linear_direct_kernel<T, 64, 64, 2, 2>), grid, dim3(256), 0, st, a);
+            if (tile == 256) hipLaunchKernelGGL((linear_direct_kernel<T, 256, 256, 2, 4, 32, 4>), grid, dim3(512), 0, st, a);
+            else if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<T, 128, 128, 2, 2, 64, 4>), grid, dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((linear_direct_kernel<T, 64, 64, 2, 2, 64, 4>), grid, dim3(256), 0, st, a);
             WPK_HIP(hipGetLastError());
             return WPK_OK;
         }
