@@ -219,41 +219,70 @@ template <> struct TileType<float> {
 // numbers still; what overflows by that shows in the sums, and is summed again as it stands.
 static const float kSplitScale = 65536.0f;
 
-// A wave's blocks go to y through LDS, 32 rows at a time, so that y is written (and the residual read) in whole lines and what
-// follows the sums stands in the code once.  `odd`: the sums are not to be used, they are formed again one by one in fp32.
+// A wave's blocks go to y through LDS, 32 rows at a time, so that y is written (and the residual read) in whole lines.  What
+// follows the sums but for the residual stands in the code once, in a loop over LDS; the residual's loads go out before.
+// `odd`: the sums are not to be used, they are formed again one by one in fp32.
 template <typename T, int TM, int TN>
 __device__ inline void put_tile(const LinearArgs &a, const f32x16 (&acc)[TM][TN], float *rows, float scale, bool odd, int slice,
                                 int k_begin, int k_end, int m0, int n0)
 {
-    const int kCols = 32 * TN, kPitch = kCols + 4, kQuads = kCols / 4;
+    typedef T tvec __attribute__((ext_vector_type(4)));
+    const int kCols = 32 * TN, kPitch = kCols + 4, kQuads = kCols / 4, kStep = 64 / kQuads, kTurns = 32 / kStep;
     const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
+    const int n = n0 + lane % kQuads * 4, n_in = min(n, max(a.n - 4, 0));    // the lane's columns, and ones that there are
+    const bool wide = a.wide_y && a.slices == 1, has_n = n < a.n;
+    f32x4 bias = {0, 0, 0, 0};
+    if (a.bias && wide) bias = __builtin_convertvector(*(const tvec *)((const T *)a.bias + n_in), f32x4);
+    float *const mine = rows + lane / kQuads * kPitch + lane % kQuads * 4;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
+        const int m = m0 + i * 32 + lane / kQuads;
+        tvec res[kTurns];
+        if (a.residual && wide)
+#pragma unroll
+            for (int t = 0; t < kTurns; ++t)
+                res[t] = *(const tvec *)((const T *)a.residual + (int64_t)min(m + t * kStep, a.m - 1) * a.residual_stride + n_in);
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int r = 0; r < 16; r += 4)
                 *(f32x4 *)&rows[row * kPitch + 32 * j + 2 * r + 4 * half] =
-                    f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
+                    f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]} * scale;
+        if (sizeof(T) == 4 && odd) {
 #pragma unroll 1
-        for (int t = lane; t < 32 * kQuads; t += 64) {
-            const int m = m0 + i * 32 + t / kQuads, n = n0 + t % kQuads * 4;
-            f32x4 v = *(const f32x4 *)&rows[t / kQuads * kPitch + t % kQuads * 4] * scale;
-            if (sizeof(T) == 4 && odd) {
-                const T *const xr = (const T *)a.x + (int64_t)min(m, a.m - 1) * a.x_stride;
+            for (int e = lane; e < 32 * kCols; e += 64) {
+                const T *const xr = (const T *)a.x + (int64_t)min(m0 + i * 32 + e / kCols, a.m - 1) * a.x_stride;
+                const T *const wr = (const T *)a.w + (int64_t)min(n0 + e % kCols, a.n - 1) * a.w_stride;
+                float sum = 0.0f;
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    const T *const wr = (const T *)a.w + (int64_t)min(n + c, a.n - 1) * a.w_stride;
-                    float sum = 0.0f;
-#pragma unroll 1
-                    for (int k = k_begin; k < k_end; ++k) sum = fmaf((float)xr[k], (float)wr[k], sum);
-                    v[0] = c == 0 ? sum : v[0];
-                    v[1] = c == 1 ? sum : v[1];
-                    v[2] = c == 2 ? sum : v[2];
-                    v[3] = c == 3 ? sum : v[3];
-                }
+                for (int k = k_begin; k < k_end; ++k) sum = fmaf((float)xr[k], (float)wr[k], sum);
+                rows[e / kCols * kPitch + e % kCols] = sum;
             }
-            finish_or_part<T>(a, slice, m, n, v);
+        }
+        if (!wide) {
+#pragma unroll 1
+            for (int t = 0; t < kTurns; ++t)
+                finish_or_part<T>(a, slice, m + t * kStep, n, *(const f32x4 *)(mine + t * kStep * kPitch));
+            continue;
+        }
+        if (a.act != WPK_ACT_NONE) {
+#pragma unroll 1
+            for (int t = 0; t < kTurns; ++t) {
+                f32x4 v = *(const f32x4 *)(mine + t * kStep * kPitch) + bias;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] = a.y_f32 ? apply_act<float>(v[c], a.act) : apply_act<T>(v[c], a.act);
+                *(f32x4 *)(mine + t * kStep * kPitch) = v;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            f32x4 v = *(const f32x4 *)(mine + t * kStep * kPitch);
+            if (a.act == WPK_ACT_NONE) v += bias;
+            if (a.residual) v += __builtin_convertvector(res[t], f32x4);
+            if (!has_n || m + t * kStep >= a.m) continue;
+            const int64_t at = (int64_t)(m + t * kStep) * a.y_stride + n;
+            if (sizeof(T) == 4 || a.y_f32) *(f32x4 *)((float *)a.y + at) = v;
+            else *(tvec *)((T *)a.y + at) = __builtin_convertvector(v, tvec);
         }
     }
 }
@@ -367,7 +396,7 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
 // ahead of the products.  A wave's load brings 1024 bytes of whole rows.  The 16-byte pieces of a row stand in the order of their
 // number xor some bits of the row's, which the lanes bring about by what they ask for: the lanes that read the same piece of
 // 32 rows take all banks alike.
-template <typename T, int BM, int BN, int WM, int WN, int BK, int STAGES> __global__ void __launch_bounds__(64 * WM * WN, 2)
+template <typename T, int BM, int BN, int WM, int WN, int BK, int STAGES> __global__ void __launch_bounds__(64 * WM * WN, BM == 256 ? 2 : 1)
 linear_direct_kernel(LinearArgs a)
 {
     typedef typename Mma<T>::v8 v8;
@@ -418,29 +447,48 @@ linear_direct_kernel(LinearArgs a)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-    // Steps behind the last are asked for as well, all of them outside, so that the same number of loads is always under way.
-#pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) fetch(s, k_begin + s * BK);
-    int stage = 0;
-    for (int k = k_begin; k < k_end; k += BK) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * kLoads) : "memory");
-        __builtin_amdgcn_s_barrier();        // this step's operands are there, and nobody reads the last step's any more
-        const int behind = stage == 0 ? STAGES - 1 : stage - 1;
-        fetch(behind, k + (STAGES - 1) * BK);
+    // A step's blocks of 16 entries are read one ahead of the products, the first of a step with the last products of the step
+    // before: between them all waves meet, the step's operands there and the buffer before it read by everyone, and the loads
+    // of the step STAGES later go out into that.  Steps behind the last are asked for as well, all of them outside, so that
+    // the same number of loads is always under way.
+    const int kBlocks = BK / 16;
+    static_assert(kBlocks % 2 == 0, "blocks alternate between two sets of registers");
+    v8 fw[2][TN], fx[2][TM];
+    auto read_block = [&](int stage, int s) {
         const T *const pw = &lds[stage][wn * TN * 32 * BK], *const px = &lds[stage][(BN + wm * TM * 32) * BK];
 #pragma unroll
-        for (int s = 0; s < BK / 16; ++s) {
-            v8 fw[TN], fx[TM];
+        for (int j = 0; j < TN; ++j) fw[s & 1][j] = *(const v8 *)(pw + read[s] + j * 32 * BK);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fw[j] = *(const v8 *)(pw + read[s] + j * 32 * BK);
+        for (int i = 0; i < TM; ++i) fx[s & 1][i] = *(const v8 *)(px + read[s] + i * 32 * BK);
+    };
+    auto multiply = [&](int s) {
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fx[i] = *(const v8 *)(px + read[s] + i * 32 * BK);
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+            for (int j = 0; j < TN; ++j) acc[i][j] = Mma<T>::m32(fw[s & 1][j], fx[s & 1][i], acc[i][j]);
+    };
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = Mma<T>::m32(fw[j], fx[i], acc[i][j]);
+    for (int s = 0; s < STAGES; ++s) fetch(s, k_begin + s * BK);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * kLoads) : "memory");
+    __builtin_amdgcn_s_barrier();
+    read_block(0, 0);
+    int stage = 0;
+    for (int k = k_begin; k < k_end; k += BK) {
+        const int next = stage == STAGES - 1 ? 0 : stage + 1;
+#pragma unroll
+        for (int s = 0; s < kBlocks; ++s) {
+            if (s + 1 < kBlocks) {
+                read_block(stage, s + 1);
+            } else {
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * kLoads) : "memory");
+                __builtin_amdgcn_s_barrier();
+                fetch(stage, k + STAGES * BK);
+                read_block(next, 0);
+            }
+            multiply(s);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        stage = stage == STAGES - 1 ? 0 : stage + 1;
+        stage = next;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the loads of zeros write LDS too)
     __syncthreads();
@@ -512,7 +560,7 @@ template <typename T> static int launch_tiles(const LinearArgs &a, int tile, boo
     const dim3 grid(tile_count(a, tile), a.slices);
     if constexpr (sizeof(T) == 2) {
         if (direct) {
-            if (tile == 256) hipLaunchKernelGGL((linear_direct_kernel<T, 256, 256, 2, 4, 32, 4>), grid, dim3(512), 0, st, a);
+            if (tile == 256) hipLaunchKernelGGL((linear_direct_kernel<T, 256, 256, 2, 4, 64, 2>), grid, dim3(512), 0, st, a);
             else if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<T, 128, 128, 2, 2, 64, 4>), grid, dim3(256), 0, st, a);
             else hipLaunchKernelGGL((linear_direct_kernel<T, 64, 64, 2, 2, 64, 4>), grid, dim3(256), 0, st, a);
             WPK_HIP(hipGetLastError());
