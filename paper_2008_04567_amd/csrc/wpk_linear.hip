@@ -17,6 +17,7 @@ struct LinearArgs {
     float *part;                      // partial products [slice][m][part_stride], where the reduction is cut
     int32_t m, n, k, act, y_f32;
     int32_t slices, slice_k;          // reduction entries of a slice (a multiple of 64)
+    int32_t width;                    // columns of a workgroup of the row kernel (a multiple of four)
     int32_t wide_y;                   // rows of y (and the residual, the bias) hold whole aligned groups of four
     int64_t x_stride, w_stride, y_stride, residual_stride, part_stride;
 };
@@ -107,20 +108,20 @@ template <typename T> __global__ void __launch_bounds__(256) linear_join_kernel(
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------
-// A workgroup of eight waves owns 16 NT columns of y and all of up to 16 MT rows.  A wave takes every eighth run of 64
-// reduction entries (a line of a row of w in 16-bit types) of its slice and keeps U of them in flight.  Rows beyond the
-// matrices are read as the last one; nothing of them is stored.
+// A workgroup of eight waves owns `width` columns of y, 16 NT at most, and all of up to 16 MT rows.  A wave takes every eighth run
+// of 64 reduction entries (a line of a row of w in 16-bit types) of its slice and keeps U of them in flight.  Rows beyond the
+// matrices or the width are read as the last one (lines that are on their way already); nothing of them is stored.
 static const int kRowsWaves = 8;
 template <typename T, int MT, int NT, int U> __global__ void __launch_bounds__(64 * kRowsWaves) linear_rows_kernel(LinearArgs a)
 {
     typedef typename Mma<T>::v8 v8;
     __shared__ __align__(16) f32x4 sums[kRowsWaves][MT * NT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 16 * NT, slice = blockIdx.y;
+    const int n0 = blockIdx.x * a.width, n_end = min(n0 + a.width, a.n), slice = blockIdx.y;
     const int k_end = min(a.k, (slice + 1) * a.slice_k), k_begin = slice * a.slice_k + 64 * wave;
     const T *wp[NT], *xp[MT];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) wp[i] = (const T *)a.w + (int64_t)min(n0 + 16 * i + row, a.n - 1) * a.w_stride + 8 * g;
+    for (int i = 0; i < NT; ++i) wp[i] = (const T *)a.w + (int64_t)min(n0 + 16 * i + row, n_end - 1) * a.w_stride + 8 * g;
 #pragma unroll
     for (int i = 0; i < MT; ++i) xp[i] = (const T *)a.x + (int64_t)min(16 * i + row, a.m - 1) * a.x_stride + 8 * g;
     f32x4 acc[MT][NT];
@@ -188,7 +189,8 @@ template <typename T, int MT, int NT, int U> __global__ void __launch_bounds__(6
         f32x4 v = sums[0][t][lane];
 #pragma unroll
         for (int s = 1; s < kRowsWaves; ++s) v += sums[s][t][lane];
-        finish_or_part<T>(a, slice, 16 * (t / NT) + row, n0 + 16 * (t % NT) + 4 * g, v);
+        const int n = n0 + 16 * (t % NT) + 4 * g;
+        if (n < n_end) finish_or_part<T>(a, slice, 16 * (t / NT) + row, n, v);
     }
 }
 
@@ -287,8 +289,10 @@ __device__ inline void put_tile(const LinearArgs &a, const f32x16 (&acc)[TM][TN]
     }
 }
 
-// BM rows of y (columns of the MFMA) by BN columns, WM x WN waves of 32 x 32 blocks.  Operands of the step after the next
-// ... are held in registers while a step's are multiplied, and stored to the other LDS buffer.
+// BM rows of y (columns of the MFMA) by BN columns, WM x WN waves of 32 x 32 blocks.  A step's operands are held in registers
+// while the step before is multiplied, and go to LDS (fp32's cut into their parts on the way) between two meetings of the
+// waves.  One LDS buffer: workgroups that share a compute unit fill each other's pauses, which for fp32, whose cutting takes
+// two thirds of the products' time, was worth more than a second buffer.
 template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN) linear_tiles_kernel(LinearArgs a)
 {
     typedef typename TileType<T>::part_t part_t;
@@ -296,8 +300,10 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
     const int NP = TileType<T>::parts, BK = TileType<T>::bk, kRow = BK + 8, kThreads = 64 * WM * WN;
     const int TM = BM / WM / 32, TN = BN / WN / 32, kOctets = BK / 8, kPer = (BM + BN) * kOctets / kThreads;
     static_assert((BM + BN) * kOctets % kThreads == 0 && BN * kOctets % kThreads == 0, "whole rounds of loads");
-    __shared__ __align__(16) part_t lds[2][NP][(BM + BN) * kRow];      // rows of w, then rows of x
-    static_assert(sizeof(lds) >= sizeof(float) * WM * WN * 32 * (32 * TN + 4), "what put_tile needs");
+    const int kPutBytes = 4 * WM * WN * 32 * (32 * TN + 4), kBytes = (BM + BN) * kRow * NP * (int)sizeof(part_t);
+    __shared__ __align__(16) unsigned char shared[kBytes > kPutBytes ? kBytes : kPutBytes];
+    part_t *const lds = (part_t *)shared;              // [part][rows of w, then rows of x][kRow]
+    const int kPart = (BM + BN) * kRow;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 31, half = lane >> 5;
     const int wm = wave % WM, wn = wave / WM, slice = blockIdx.y;
     const TileAt at = tile_of(blockIdx.x, (a.m + BM - 1) / BM, (a.n + BN - 1) / BN);
@@ -316,26 +322,9 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
         if (k + BK <= k_end) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) held[i] = Octet<T>::load(src[i] + k);
-        } else {
+        } else if (k < k_end) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) held[i] = Octet<T>::load_some(src[i] + k, k_end - k - (tid + i * kThreads) % kOctets * 8);
-        }
-    };
-    auto stage = [&](int buf) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int task = tid + i * kThreads, to = task / kOctets * kRow + task % kOctets * 8;
-            if constexpr (NP == 1) {
-                *(p8 *)&lds[buf][0][to] = held[i];
-            } else {
-                f32x8 v = held[i] * kSplitScale;
-#pragma unroll
-                for (int q = 0; q < NP; ++q) {
-                    const p8 u = __builtin_convertvector(v, p8);
-                    v -= __builtin_convertvector(u, f32x8);
-                    *(p8 *)&lds[buf][q][to] = u;
-                }
-            }
         }
     };
     f32x16 acc[TM][TN];
@@ -347,21 +336,33 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
     fetch(k_begin);
-    stage(0);
-    __syncthreads();
-    int buf = 0;
-    for (int k = k_begin; k < k_end; k += BK, buf ^= 1) {
-        const bool more = k + BK < k_end;
-        if (more) fetch(k + BK);
+    for (int k = k_begin; k < k_end; k += BK) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int task = tid + i * kThreads, to = task / kOctets * kRow + task % kOctets * 8;
+            if constexpr (NP == 1) {
+                *(p8 *)&lds[to] = held[i];
+            } else {
+                f32x8 v = held[i] * kSplitScale;
+#pragma unroll
+                for (int q = 0; q < NP; ++q) {
+                    const p8 u = __builtin_convertvector(v, p8);
+                    v -= __builtin_convertvector(u, f32x8);
+                    *(p8 *)&lds[q * kPart + to] = u;
+                }
+            }
+        }
+        __syncthreads();
+        fetch(k + BK);
 #pragma unroll
         for (int s = 0; s < BK / 16; ++s) {
             p8 fw[TN][NP], fx[TM][NP];
 #pragma unroll
             for (int q = 0; q < NP; ++q) {
 #pragma unroll
-                for (int j = 0; j < TN; ++j) fw[j][q] = *(const p8 *)&lds[buf][q][(wn * TN * 32 + j * 32 + row) * kRow + 16 * s + 8 * half];
+                for (int j = 0; j < TN; ++j) fw[j][q] = *(const p8 *)&lds[q * kPart + (wn * TN * 32 + j * 32 + row) * kRow + 16 * s + 8 * half];
 #pragma unroll
-                for (int i = 0; i < TM; ++i) fx[i][q] = *(const p8 *)&lds[buf][q][(BN + wm * TM * 32 + i * 32 + row) * kRow + 16 * s + 8 * half];
+                for (int i = 0; i < TM; ++i) fx[i][q] = *(const p8 *)&lds[q * kPart + (BN + wm * TM * 32 + i * 32 + row) * kRow + 16 * s + 8 * half];
             }
 #pragma unroll
             for (int u = 0; u < NP; ++u)
@@ -372,7 +373,6 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
 #pragma unroll
                         for (int j = 0; j < TN; ++j) acc[i][j] = Mma<part_t>::m32(fw[j][u], fx[i][v], acc[i][j]);
         }
-        if (more) stage(buf ^ 1);
         __syncthreads();
     }
 
@@ -388,7 +388,7 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
                 for (int r = 0; r < 16; ++r) odd = odd || !(fabsf(acc[i][j][r]) <= 3.4028234e38f);
         odd = __any(odd);
     }
-    put_tile<T, TM, TN>(a, acc, (float *)&lds[0][0][0] + wave * 32 * (32 * TN + 4), scale, odd, slice, k_begin, k_end,
+    put_tile<T, TM, TN>(a, acc, (float *)shared + wave * 32 * (32 * TN + 4), scale, odd, slice, k_begin, k_end,
                         m0 + wm * TM * 32, n0 + wn * TN * 32);
 }
 
@@ -500,16 +500,24 @@ linear_direct_kernel(LinearArgs a)
 static const int kRowsMost = 64;      // rows of x that the row kernel takes
 struct LinearShape {
     int tile;                         // rows and columns of a tile; 0: the row kernel
+    int width;                        // of a workgroup of the row kernel
     int slices, slice_k;
 };
 
 static LinearShape linear_shape(const wpk_linear_desc &d)
 {
-    LinearShape s = {0, 1, (d.k + 63) / 64 * 64};
+    LinearShape s = {0, 0, 1, (d.k + 63) / 64 * 64};
     const int64_t steps = (d.k + 63) / 64;
     int64_t groups, slices;
     if (d.m <= kRowsMost) {
-        groups = (d.n + 15) / 16;
+        // As many columns a workgroup as give every compute unit the same: 8512 columns of 2048 by 32 rows take 16.9 us in
+        // workgroups of 32 (266 for 256 compute units) and 10.5 in such of 36.  At least as many as keep the reads of x, all
+        // of which every workgroup does, small beside those of w.
+        const int least = d.m <= 4 ? 4 : d.m <= 16 ? 8 : 16;
+        const int64_t rounds = ((int64_t)d.n + 48 * kComputeUnits - 1) / (48 * kComputeUnits);
+        const int64_t even = (d.n + rounds * kComputeUnits - 1) / (rounds * kComputeUnits);
+        s.width = (int)((even > least ? even : least) + 3) / 4 * 4;
+        groups = (d.n + s.width - 1) / s.width;
         // each of the eight waves keeps four runs of 64 at least
         slices = kComputeUnits / groups;
         if (slices > steps / (4 * kRowsWaves)) slices = steps / (4 * kRowsWaves);
@@ -517,7 +525,8 @@ static LinearShape linear_shape(const wpk_linear_desc &d)
         auto tiles = [&](int t) { return (int64_t)((d.m + t - 1) / t) * ((d.n + t - 1) / t); };
         s.tile = d.dtype != WPK_F32 && tiles(256) >= kComputeUnits ? 256 : tiles(128) >= kComputeUnits / 2 ? 128 : 64;
         groups = tiles(s.tile);
-        slices = kComputeUnits / groups;
+        // fp32 wants several workgroups a compute unit, which cut their operands while others multiply
+        slices = (d.dtype != WPK_F32 ? 1 : s.tile == 64 ? 3 : 2) * kComputeUnits / groups;
         if (slices > steps / 8) slices = steps / 8;
     }
     if (slices > 16) slices = 16;
@@ -542,15 +551,20 @@ static int check_linear(const wpk_linear_desc *dp)
     return WPK_OK;
 }
 
-template <typename T> static int launch_rows(const LinearArgs &a, hipStream_t st)
+template <typename T, int MT> static int launch_rows(const LinearArgs &a, hipStream_t st)
 {
-    const int kThreads = 64 * kRowsWaves;
-    const dim3 grid((a.n + 15) / 16, a.slices);
-    if (a.m <= 16) hipLaunchKernelGGL((linear_rows_kernel<T, 1, 1, 4>), grid, dim3(kThreads), 0, st, a);
-    else if (a.m <= 32) hipLaunchKernelGGL((linear_rows_kernel<T, 2, 1, 2>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((linear_rows_kernel<T, 4, 1, 1>), grid, dim3(kThreads), 0, st, a);
+    const int kThreads = 64 * kRowsWaves, U = MT == 1 ? (sizeof(T) == 2 ? 4 : 2) : MT == 2 || sizeof(T) == 2 ? 2 : 1;
+    const dim3 grid((a.n + a.width - 1) / a.width, a.slices);
+    if (a.width <= 16) hipLaunchKernelGGL((linear_rows_kernel<T, MT, 1, U>), grid, dim3(kThreads), 0, st, a);
+    else if (a.width <= 32) hipLaunchKernelGGL((linear_rows_kernel<T, MT, 2, U>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((linear_rows_kernel<T, MT, 3, U>), grid, dim3(kThreads), 0, st, a);
     WPK_HIP(hipGetLastError());
     return WPK_OK;
+}
+
+template <typename T> static int launch_rows(const LinearArgs &a, hipStream_t st)
+{
+    return a.m <= 16 ? launch_rows<T, 1>(a, st) : a.m <= 32 ? launch_rows<T, 2>(a, st) : launch_rows<T, 4>(a, st);
 }
 
 static unsigned tile_count(const LinearArgs &a, int b) { return (unsigned)(((a.m + b - 1) / b) * ((a.n + b - 1) / b)); }
@@ -613,7 +627,7 @@ int wpk_linear_fwd(const wpk_linear_desc *dp, const void *x, const void *w, cons
     const bool wide = d.n % 4 == 0 && d.y_stride % 4 == 0 && aligned_to(y, 4 * ye) && aligned_to(bias, 4 * e) &&
                       (!residual || (d.residual_stride % 4 == 0 && aligned_to(residual, 4 * e)));
     LinearArgs a = {x, w, bias, residual, y, (float *)workspace, d.m, d.n, d.k, d.act, d.y_dtype == WPK_F32,
-                    s.slices, s.slice_k, wide, d.x_stride, d.w_stride, d.y_stride, d.residual_stride, part_stride(d)};
+                    s.slices, s.slice_k, s.width, wide, d.x_stride, d.w_stride, d.y_stride, d.residual_stride, part_stride(d)};
     // (loads that write LDS move 16 aligned bytes)
     const bool direct = d.k % 8 == 0 && d.x_stride % 8 == 0 && d.w_stride % 8 == 0 && aligned_to(x, 16) && aligned_to(w, 16);
     const hipStream_t st = (hipStream_t)stream;
