@@ -318,25 +318,7 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
                         : (const T *)a.x + (int64_t)min(m0 + r - BN, a.m - 1) * a.x_stride + 8 * o;
     }
     typename Mma<T>::v8 held[kPer];
-    auto fetch = [&](int k) {
-        if (k + BK <= k_end) {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) held[i] = Octet<T>::load(src[i] + k);
-        } else if (k < k_end) {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) held[i] = Octet<T>::load_some(src[i] + k, k_end - k - (tid + i * kThreads) % kOctets * 8);
-        }
-    };
-    f32x16 acc[TM][TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-
-    fetch(k_begin);
-    for (int k = k_begin; k < k_end; k += BK) {
+    auto stage = [&]() {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int task = tid + i * kThreads, to = task / kOctets * kRow + task % kOctets * 8;
@@ -352,8 +334,16 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
                 }
             }
         }
-        __syncthreads();
-        fetch(k + BK);
+    };
+    f32x16 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+    auto multiply = [&]() {
 #pragma unroll
         for (int s = 0; s < BK / 16; ++s) {
             p8 fw[TN][NP], fx[TM][NP];
@@ -373,6 +363,29 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
 #pragma unroll
                         for (int j = 0; j < TN; ++j) acc[i][j] = Mma<part_t>::m32(fw[j][u], fx[i][v], acc[i][j]);
         }
+    };
+    // whole steps, the next one's loads under way without a branch around them (the last whole one's again behind it)
+    const int k_whole = k_begin + (k_end - k_begin) / BK * BK;
+    if (k_whole > k_begin) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) held[i] = Octet<T>::load(src[i] + k_begin);
+        for (int k = k_begin; k < k_whole; k += BK) {
+            stage();
+            __syncthreads();
+            const int next = min(k + BK, k_whole - BK);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) held[i] = Octet<T>::load(src[i] + next);
+            multiply();
+            __syncthreads();
+        }
+    }
+    if (k_whole < k_end) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            held[i] = Octet<T>::load_some(src[i] + k_whole, k_end - k_whole - (tid + i * kThreads) % kOctets * 8);
+        stage();
+        __syncthreads();
+        multiply();
         __syncthreads();
     }
 
