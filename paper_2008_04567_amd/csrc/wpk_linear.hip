@@ -268,7 +268,7 @@ __device__ inline void put_tile(const LinearArgs &a, const f32x16 (&acc)[TM][TN]
             continue;
         }
         if (a.act != WPK_ACT_NONE) {
-#pragma unroll 1
+#pragma unroll sizeof(T) == 2 ? 4 : 1
             for (int t = 0; t < kTurns; ++t) {
                 f32x4 v = *(const f32x4 *)(mine + t * kStep * kPitch) + bias;
 #pragma unroll
@@ -409,7 +409,8 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
 // ahead of the products.  A wave's load brings 1024 bytes of whole rows.  The 16-byte pieces of a row stand in the order of their
 // number xor some bits of the row's, which the lanes bring about by what they ask for: the lanes that read the same piece of
 // 32 rows take all banks alike.
-template <typename T, int BM, int BN, int WM, int WN, int BK, int STAGES> __global__ void __launch_bounds__(64 * WM * WN, BM == 256 ? 2 : 1)
+template <typename T, int BM, int BN, int WM, int WN, int BK, int STAGES>
+__global__ void __launch_bounds__(64 * WM * WN, (BM + BN) * BK * STAGES * 2 > 81920 ? WM * WN / 4 : WM * WN / 2)
 linear_direct_kernel(LinearArgs a)
 {
     typedef typename Mma<T>::v8 v8;
@@ -588,7 +589,10 @@ template <typename T> static int launch_tiles(const LinearArgs &a, int tile, boo
     if constexpr (sizeof(T) == 2) {
         if (direct) {
             if (tile == 256) hipLaunchKernelGGL((linear_direct_kernel<T, 256, 256, 2, 4, 64, 2>), grid, dim3(512), 0, st, a);
-            else if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<T, 128, 128, 2, 2, 64, 4>), grid, dim3(256), 0, st, a);
+            // four steps' operands in LDS for a workgroup that has its compute unit to itself, two for two that share one
+            else if (tile == 128 && grid.x * grid.y <= (unsigned)kComputeUnits)
+                hipLaunchKernelGGL((linear_direct_kernel<T, 128, 128, 2, 4, 64, 4>), grid, dim3(512), 0, st, a);
+            else if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<T, 128, 128, 2, 4, 64, 2>), grid, dim3(512), 0, st, a);
             else hipLaunchKernelGGL((linear_direct_kernel<T, 64, 64, 2, 2, 64, 4>), grid, dim3(256), 0, st, a);
             WPK_HIP(hipGetLastError());
             return WPK_OK;
