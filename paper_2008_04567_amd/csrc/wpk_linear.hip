@@ -407,8 +407,8 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
 
 // The same for 16-bit operands in aligned rows: loads write LDS directly and take no registers, STAGES - 1 steps of BK entries
 // ahead of the products.  A wave's load brings 1024 bytes of whole rows.  The 16-byte pieces of a row stand in the order of their
-// number xor some bits of the row's, which the lanes bring about by what they ask for: the lanes that read the same piece of
-// 32 rows take all banks alike.
+// number xor some bits of the row's, which the lanes bring about by what they ask for: 16 lanes that read the same piece of
+// neighbouring rows take all banks.
 template <typename T, int BM, int BN, int WM, int WN, int BK, int STAGES>
 __global__ void __launch_bounds__(64 * WM * WN, (BM + BN) * BK * STAGES * 2 > 81920 ? WM * WN / 4 : WM * WN / 2)
 linear_direct_kernel(LinearArgs a)
@@ -424,25 +424,26 @@ linear_direct_kernel(LinearArgs a)
     const TileAt at = tile_of(blockIdx.x, (a.m + BM - 1) / BM, (a.n + BN - 1) / BN);
     const int m0 = at.m * BM, n0 = at.n * BN;
     const int k_begin = slice * a.slice_k, k_end = min(a.k, k_begin + a.slice_k);
-    auto order = [](int r) { return BK == 64 ? r & 7 : (r >> 2) & 3; };
+    auto order = [](int r) { return BK == 64 ? (r >> 1) & 7 : (r >> 2) & 3; };
 
     const int w_loads = BN / kLoadRows, load_row = lane / kPieces;
     const bool of_w = wave * kLoads < w_loads;
     const int r0 = (of_w ? n0 : m0) + (wave * kLoads - (of_w ? 0 : w_loads)) * kLoadRows, last = (of_w ? a.n : a.m) - 1;
     const int64_t stride = of_w ? a.w_stride : a.x_stride;
-    const int base = min(r0, last), piece = (lane % kPieces ^ order(load_row)) * 8;
+    const int base = min(r0, last);
     const Rows src = __builtin_amdgcn_make_buffer_rsrc((T *)(of_w ? a.w : a.x) + base * stride, 0, 0x7fffffff, 0x00020000);
+    auto piece = [&](int i) { return (lane % kPieces ^ order(kLoadRows * (i & 1) + load_row)) * 8; };
     uint32_t from[kLoads];                                     // rows beyond the matrix are read as its last one
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-        from[i] = (uint32_t)((min(r0 + kLoadRows * i + load_row, last) - base) * (int)stride + piece) * sizeof(T);
+        from[i] = (uint32_t)((min(r0 + kLoadRows * i + load_row, last) - base) * (int)stride + piece(i)) * sizeof(T);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)&lds[0][0] + wave * kLoads * 1024;
     auto fetch = [&](int stage, int k) {
         const uint32_t to = lds0 + stage * (uint32_t)sizeof(lds[0]);
         const bool whole = k + BK <= k_end;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const uint32_t off = whole || k + piece < k_end ? from[i] : kOutside;      // (outside: zeros)
+            const uint32_t off = whole || k + piece(i) < k_end ? from[i] : kOutside;      // (outside: zeros)
             asm volatile("s_mov_b32 m0, %2\n s_nop 0\n buffer_load_dwordx4 %0, %1, %3 offen lds"
                          :
                          : "v"(off), "s"(src), "s"(to + i * 1024), "s"(k * (uint32_t)sizeof(T))
