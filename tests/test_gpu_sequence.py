@@ -25,6 +25,18 @@ def test_linear_sizes(S, dtype, m, n, k):
     S.run_linear(m, n, k, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("m,n,k,y_f32", [(4097, 4100, 72, False), (4100, 4097, 200, True), (4096, 4352, 64, False), (8200, 2050, 136, False)])
+def test_linear_many_large_tiles(S, dtype, m, n, k, y_f32):
+    S.run_linear(m, n, k, dtype, act="silu", y_f32=y_f32)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,n,k", [(2, 9000, 64), (20, 13000, 72), (50, 20000, 40), (64, 12290, 130), (3000, 1500, 24), (2000, 2300, 8)])
+def test_linear_wide_outputs(S, dtype, m, n, k):
+    S.run_linear(m, n, k, dtype, act="relu")
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("m,n,k", [(3, 70, 37), (20, 33, 129), (130, 190, 201), (300, 290, 515)])
 def test_linear_odd_reduction_and_unaligned_rows(S, dtype, m, n, k):
