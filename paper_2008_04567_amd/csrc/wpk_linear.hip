@@ -68,20 +68,18 @@ template <typename T, typename Y> __device__ inline void finish(const LinearArgs
     const T *const r = (const T *)a.residual + (int64_t)m * a.residual_stride + n, *const b = (const T *)a.bias + n;
     if (a.wide_y) {
         if (a.bias) v += __builtin_convertvector(*(const tvec *)b, f32x4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = apply_act<Y>(v[i], a.act);
+        v = apply_act<Y>(v, a.act);
         if (a.residual) v += __builtin_convertvector(*(const tvec *)r, f32x4);
         *(yvec *)y = __builtin_convertvector(v, yvec);
     } else {
+        const int left = min(4, a.n - n);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (n + i >= a.n) break;
-            float s = v[i];
-            if (a.bias) s += (float)b[i];
-            s = apply_act<Y>(s, a.act);
-            if (a.residual) s += (float)r[i];
-            y[i] = (Y)s;
-        }
+        for (int i = 0; i < 4; ++i)
+            if (a.bias && i < left) v[i] += (float)b[i];
+        v = apply_act<Y>(v, a.act);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) y[i] = (Y)(a.residual ? v[i] + (float)r[i] : v[i]);
     }
 }
 template <typename T> __device__ inline void finish(const LinearArgs &a, int m, int n, f32x4 v)
@@ -268,11 +266,10 @@ __device__ inline void put_tile(const LinearArgs &a, const f32x16 (&acc)[TM][TN]
             continue;
         }
         if (a.act != WPK_ACT_NONE) {
-#pragma unroll sizeof(T) == 2 ? 4 : 1
+#pragma unroll 1
             for (int t = 0; t < kTurns; ++t) {
                 f32x4 v = *(const f32x4 *)(mine + t * kStep * kPitch) + bias;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] = a.y_f32 ? apply_act<float>(v[c], a.act) : apply_act<T>(v[c], a.act);
+                v = a.y_f32 ? apply_act<float>(v, a.act) : apply_act<T>(v, a.act);
                 *(f32x4 *)(mine + t * kStep * kPitch) = v;
             }
         }

@@ -100,11 +100,19 @@ __device__ inline float erf_fast(float x)
 }
 template <typename T> __device__ inline float erf_as(float v) { return sizeof(T) == 4 ? erff(v) : erf_fast(v); }
 
-template <typename T> __device__ inline float apply_act(float v, int act)
+// the activation of four values; T: what they are rounded to next
+template <typename T> __device__ inline f32x4 apply_act(f32x4 v, int act)
 {
-    if (act == WPK_ACT_RELU) return v < 0.0f ? 0.0f : v;                  // (NaN stays)
-    if (act == WPK_ACT_SILU) return silu_as<T>(v);
-    if (act == WPK_ACT_GELU) return 0.5f * v * (1.0f + erf_as<T>(v * 0.70710678f));
+    if (act == WPK_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];         // (NaN stays)
+    } else if (act == WPK_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = silu_as<T>(v[i]);
+    } else if (act == WPK_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = 0.5f * v[i] * (1.0f + erf_as<T>(v[i] * 0.70710678f));
+    }
     return v;
 }
 
