@@ -114,6 +114,7 @@ static int scan_chunk(int dtype, int state_dim)     // tokens of a chunk (what f
 
 struct ScanShape {
     int n_parts, part_chunks;
+    bool by_length;           // requests of different lengths that do not all start at once: the longest first
 };
 
 // Requests are cut along their tokens where their heads alone would leave compute units idle.  Every part but a
@@ -127,9 +128,9 @@ static ScanShape scan_shape(const wpk_ssm_desc &d)
     int64_t parts = groups > 0 ? room / groups : 1;
     if (parts > 16) parts = 16;
     if (parts > chunks / 4) parts = chunks / 4;
-    if (parts < 2) return {1, (int)chunks};
+    if (parts < 2) return {1, (int)chunks, groups > room && d.sequences > 1 && d.sequences <= 256};
     const int64_t each = (chunks + parts - 1) / parts;
-    return {(int)((chunks + each - 1) / each), (int)each};
+    return {(int)((chunks + each - 1) / each), (int)each, false};
 }
 
 static size_t scan_part_bytes(const wpk_ssm_desc &d, const ScanShape &s)
@@ -143,6 +144,11 @@ template <typename T, int NPAD, int Q, bool WIDE> static int launch_scan_rows(co
     if (a.n_parts > 1) {
         hipLaunchKernelGGL((ssm_scan_kernel<T, NPAD, Q, false, WIDE>), dim3(heads, a.n_parts - 1, sequences), dim3(256), 0, st, a);
         WPK_HIP(hipGetLastError());
+        if (a.n_parts > 2) {
+            const dim3 grid((a.head_dim * a.state_dim + 1023) / 1024, a.heads, sequences);
+            hipLaunchKernelGGL((ssm_join_kernel<T, Q>), grid, dim3(256), 0, st, a);
+            WPK_HIP(hipGetLastError());
+        }
     }
     hipLaunchKernelGGL((ssm_scan_kernel<T, NPAD, Q, true, WIDE>), dim3(heads, a.n_parts, sequences), dim3(256), 0, st, a);
     WPK_HIP(hipGetLastError());
@@ -208,11 +214,12 @@ static int ssm_typed(const wpk_ssm_desc &d, bool step, const void *x, const void
 {
     const size_t e = sizeof(T);
     auto rows_ok = [&](const void *p, int64_t stride, int v) { return stride % v == 0 && aligned_to(p, v * e < 16 ? v * e : 16); };
-    const ScanShape shape = scan_shape(d);
+    ScanShape shape = scan_shape(d);
+    if (!rq.starts) shape.by_length = false;
     SsmArgs<T> args = {(const T *)x, (const T *)dt, (const T *)b, (const T *)c, (const T *)z, a, d_skip, dt_bias, state_in,
                        state_out, (T *)y, rq, d.heads, d.head_dim, d.groups, d.state_dim, d.dt_softplus,
                        d.x_stride, d.dt_stride, d.b_stride, d.c_stride, d.z_stride, d.y_stride,
-                       nullptr, nullptr, shape.n_parts, shape.part_chunks,
+                       nullptr, nullptr, shape.n_parts, shape.part_chunks, shape.by_length ? d.sequences : 0,
                        d.state_dim % 8 == 0 && d.head_dim % 4 == 0 && rows_ok(b, d.b_stride, 8) && rows_ok(c, d.c_stride, 8) &&
                            rows_ok(x, d.x_stride, 4) && (!z || rows_ok(z, d.z_stride, 4)) && rows_ok(y, d.y_stride, 4),
                        d.state_dim % 4 == 0 && aligned_to(state_in, 16) && aligned_to(state_out, 16)};

@@ -36,6 +36,7 @@ template <typename T> struct SsmArgs {
     float *part_decay;
     int32_t n_parts;          // parts that a request may have
     int32_t part_chunks;      // chunks of a part (the last one takes what is left)
+    int32_t sequences;        // 0 where requests are done in their order, else as many, the longest first (256 at most)
     int32_t vec_rows, vec_state;   // whether rows (of the tensors, of the states) start at multiples of 16 bytes
 };
 
@@ -85,6 +86,34 @@ template <int PARTS, typename T> __device__ inline void parts_of(T v, bf16 (&out
         out[i] = (bf16)f;
         f -= (float)out[i];
     }
+}
+
+// Number of the request that is longer than all but n (ties in their order), by one workgroup of 256 at least; `room` holds
+// 257 numbers.  Long requests that start last would leave the device to themselves at the end.
+__device__ inline int nth_longest(const Requests &q, int sequences, int n, int *room)
+{
+    const int i = threadIdx.x;
+    if (i < sequences) {
+        const int a = min(max(q.starts[i], 0), q.tokens), b = min(max(q.starts[i + 1], 0), q.tokens);
+        room[i] = max(b - a, 0);
+    }
+    __syncthreads();
+    if (i < sequences) {
+        const int mine = room[i];
+        int before = 0;
+        for (int j = 0; j < sequences; ++j) before += room[j] > mine || (room[j] == mine && j < i);
+        if (before == n) room[256] = i;
+    }
+    __syncthreads();
+    const int r = __builtin_amdgcn_readfirstlane(room[256]);
+    __syncthreads();
+    return r;
+}
+
+// a request has as many parts as it has chunks for, one at least
+template <typename T> __device__ inline int parts_of_request(const SsmArgs<T> &a, int chunks)
+{
+    return min(max((chunks + a.part_chunks - 1) / a.part_chunks, 1), a.n_parts);
 }
 
 // One part of a request: FULL computes y and the state at its end, otherwise only what its tokens add to a state.
@@ -143,13 +172,14 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
     static __device__ void run(const SsmArgs<T> &a, Shared &sm)
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g = lane >> 4;
-        const int head = blockIdx.x % a.heads, pblock = blockIdx.x / a.heads, part = blockIdx.y, r = blockIdx.z;
+        const int head = blockIdx.x % a.heads, pblock = blockIdx.x / a.heads, part = blockIdx.y;
+        const int r = a.sequences ? nth_longest(a.rq, a.sequences, blockIdx.z, (int *)&sm.bt[0][0]) : blockIdx.z;
         const int P = a.head_dim, N = a.state_dim, group = head / (a.heads / a.groups);
         int first, length;
         request_rows(a.rq, r, &first, &length);
         const int chunks = (length + Q - 1) / Q;
-        // this part's chunks; a request has as many parts as it has chunks for, one at least
-        const int parts = min(max((chunks + a.part_chunks - 1) / a.part_chunks, 1), a.n_parts);
+        // this part's chunks
+        const int parts = parts_of_request(a, chunks);
         if (FULL ? part >= parts : part >= parts - 1) return;
         const int c0 = part * a.part_chunks, c1 = part == parts - 1 ? chunks : c0 + a.part_chunks;
 
@@ -193,16 +223,16 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
                         if (n + j < N) dst[n + j] = h[i][j];
             }
         };
-        // The state before the part.  Parts meet through the workspace: entry i holds what part i's tokens leave (part 0's
-        // with the state before the request), the last entry the state before the request itself, since whoever does the
-        // last part may be writing the pool's entry already.
+        // The state before the part.  Parts meet through the workspace: entry i holds the state behind part i (what its
+        // tokens leave, until ssm_join_kernel has added what the parts before it left), the last entry the state before the
+        // request itself, since whoever does the last part may be writing the pool's entry already.
         if (part == 0) {
             if (resume) {
                 add_state(FULL && parts > 1 ? ws + (size_t)(a.n_parts - 1) * state_size : a.state_in + pool_at, 0.0f);
                 if (!FULL) put_state(ws + (size_t)(a.n_parts - 1) * state_size);
             }
         } else if (FULL) {
-            for (int i = 0; i < part; ++i) add_state(ws + (size_t)i * state_size, i ? a.part_decay[ws_head * a.n_parts + i] : 0.0f);
+            add_state(ws + (size_t)(part - 1) * state_size, 0.0f);
         }
 
         const float rate = a.a[head], skip = a.d_skip ? a.d_skip[head] : 0.0f, dt_bias = a.dt_bias ? a.dt_bias[head] : 0.0f;
@@ -563,6 +593,40 @@ ssm_scan_kernel(SsmArgs<T> a)
     typedef SsmScan<T, NPAD, Q, FULL, WIDE> Scan;
     __shared__ typename Scan::Shared sm;
     Scan::run(a, sm);
+}
+
+// From what the parts' tokens leave to the states behind the parts: entry i of the workspace += decay of part i times entry
+// i - 1, a lane to four numbers of a state.
+template <typename T, int Q> __global__ void __launch_bounds__(256) ssm_join_kernel(SsmArgs<T> a)
+{
+    const int head = blockIdx.y, r = blockIdx.z;
+    int first, length;
+    request_rows(a.rq, r, &first, &length);
+    const int parts = parts_of_request(a, (length + Q - 1) / Q);
+    const int64_t size = (int64_t)a.head_dim * a.state_dim, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (parts < 3 || at >= size) return;
+    const int64_t ws_head = (int64_t)r * a.heads + head;
+    float *const ws = a.parts + ws_head * a.n_parts * size + at;
+    const float *const decay = a.part_decay + ws_head * a.n_parts;
+    if (a.vec_state) {
+        f32x4 cur = *(const f32x4 *)ws;
+        for (int i = 1; i < parts - 1; i += 4) {
+            f32x4 e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = *(const f32x4 *)(ws + min(i + j, parts - 2) * size);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (i + j >= parts - 1) break;
+                cur = cur * decay[i + j] + e[j];
+                *(f32x4 *)(ws + (i + j) * size) = cur;
+            }
+        }
+    } else {
+        for (int c = 0; c < 4 && at + c < size; ++c) {
+            float cur = ws[c];
+            for (int i = 1; i < parts - 1; ++i) ws[i * size + c] = cur = cur * decay[i] + ws[i * size + c];
+        }
+    }
 }
 
 }  // namespace wpk
