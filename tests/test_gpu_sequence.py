@@ -323,3 +323,46 @@ def test_offsets_beyond_32_bits(S):
     B.ssm_scan_fwd(desc, x, i["dt"], i["a"], i["b"], i["c"], y, workspace=ws)
     torch.cuda.synchronize()
     assert torch.equal(out[0], y)
+
+
+# ---- all together ---------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_mixer_prompts_then_steps_agree_with_whole_prompts(S, dtype):
+    # A layer's prompts cut anywhere and continued token by token give what the whole prompts give, but for the order of
+    # sums (few rows and many are multiplied by different kernels) and the roundings that come out of it: four in a row
+    # (row, convolution, y, output), each of a unit of the type or of 2^-20 of sums of this length, and as much for what
+    # they carry on.
+    import torch
+    from paper_2008_04567_amd.mixer import Mixer
+    ty, u = S.TYPES[dtype][1], S.TYPES[dtype][2]
+    whole, cut = [Mixer(96, 4, 32, 2, 48, slots=5, dtype=ty, seed=3) for _ in range(2)]
+    lengths, first = [9, 70, 3, 141], [4, 66, 2, 100]
+    slots = S.i32([4, 0, 2, 1])
+    rows = [S.Rng(60 + i).normal((n, 96), dtype) for i, n in enumerate(lengths)]
+    p = whole.plan(4, sum(lengths), max(lengths))
+    want = whole.prompt(p, torch.cat(rows), S.i32(S.starts_of(lengths)), slots).clone()
+    want = torch.split(want, lengths)
+    part = cut.plan(4, sum(first), max(first))
+    got = [list(torch.split(cut.prompt(part, torch.cat([r[:n] for r, n in zip(rows, first)]), S.i32(S.starts_of(first)),
+                                       slots).clone(), first))]
+    # the rest of the longest as a second prompt, the others token by token
+    rest = [0, 0, 0, 30]
+    second = cut.plan(4, 30, 30)
+    more = cut.prompt(second, rows[3][100:130], S.i32(S.starts_of(rest)), slots, resume=S.i32([1, 1, 1, 1])).clone()
+    at, outs = [4, 66, 2, 130], [[got[0][i]] for i in range(4)]
+    outs[3].append(more)
+    while any(at[i] < lengths[i] for i in range(4)):
+        live = [i for i in range(4) if at[i] < lengths[i]]
+        one = cut.plan(len(live), len(live), 1)
+        h = torch.stack([rows[i][at[i]] for i in live])
+        y = cut.step(one, h, slots[live].contiguous()).clone()
+        for k, i in enumerate(live):
+            outs[i].append(y[k:k + 1])
+            at[i] += 1
+    scale = max(float(w.float().abs().max()) for w in want)
+    for i in range(4):
+        err = (torch.cat(outs[i]).float() - want[i].float()).abs().max()
+        assert float(err) <= 16 * max(u, 2.0 ** -20) * scale, "request %d differs by %.3g" % (i, float(err))
+    for a, b in ((whole.conv_state, cut.conv_state), (whole.scan_state, cut.scan_state)):
+        err = (a.float() - b.float()).abs().max() / a.float().abs().max()
+        assert float(err) <= 16 * max(u, 2.0 ** -20)
