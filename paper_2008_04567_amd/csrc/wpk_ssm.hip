@@ -9,7 +9,11 @@ static const int kMaxHeadDim = 256, kMaxStateDim = 256;
 // ---- single tokens -----------------------------------------------------------------------------------------
 // Bound by the states, read and written once: 8 bytes a state element against 5 operations.  A workgroup takes U rows a
 // lane group of one head: LPR lanes hold a row of state_dim numbers, V = 4 (16 bytes) or 1 a lane and CI times that, so
-// every lane has U loads in flight before it needs the first.
+// every lane has U loads in flight before it needs the first.  Everything goes through buffer descriptors, an absent tensor
+// being one of no bytes: a branch around loads makes the compiler wait for what is under way at its end.  The states are
+// streamed (non-temporal): they are not wanted again before the next token.
+static const int kStream = 2;         // the buffer instructions' non-temporal bit
+
 template <typename T, int V, int CI, int U> __global__ void __launch_bounds__(256, 4) ssm_step_kernel(SsmArgs<T> a, int lpr_log)
 {
     typedef float vec __attribute__((ext_vector_type(V)));
@@ -20,65 +24,65 @@ template <typename T, int V, int CI, int U> __global__ void __launch_bounds__(25
     int first, length;
     request_rows(a.rq, r, &first, &length);
     const int slot = request_slot(a.rq, r);
-    const bool resume = a.state_in && slot >= 0, leave = a.state_out && slot >= 0;
     const size_t at = ((size_t)max(slot, 0) * a.heads + head) * P * N;
-    const float *const in = a.state_in + at;
-    float *const out = a.state_out + at;
+    const Rows in = rows_at(a.state_in + at, a.state_in && slot >= 0 ? 1 : 0, P * N * 4);
+    const Rows out = rows_at(a.state_out + at, a.state_out && slot >= 0 ? 1 : 0, P * N * 4);
+    auto offset = [&](int u, int i) -> uint32_t {                   // rows beyond the head are beyond its bytes
+        const int n = at_n + i * V * lpr;
+        return n < N ? (uint32_t)((p0 + u * rows) * N + n) * 4 : kOutside;
+    };
     vec h[U][CI];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int i = 0; i < CI; ++i) {
-            const int p = p0 + u * rows, n = at_n + i * V * lpr;
-            h[u][i] = vec(0.0f);
-            if (resume && p < P && n < N) h[u][i] = __builtin_nontemporal_load((const vec *)(in + (unsigned)(p * N + n)));
+            if constexpr (V == 4) h[u][i] = __builtin_bit_cast(vec, __builtin_amdgcn_raw_buffer_load_b128(in, offset(u, i), 0, kStream));
+            else h[u][i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(in, offset(u, i), 0, kStream));
         }
+    const uint32_t e = sizeof(T);
     const int group = head / (a.heads / a.groups);
-    const Rows brows = rows_at(a.b + (int64_t)first * a.b_stride + group * N, 1, N * (uint32_t)sizeof(T));
-    const Rows crows = rows_at(a.c + (int64_t)first * a.c_stride + group * N, 1, N * (uint32_t)sizeof(T));
-    const T *const xp = a.x + (int64_t)first * a.x_stride + (int64_t)head * P;
-    const T *const zp = a.z + (int64_t)first * a.z_stride + (int64_t)head * P;
-    T *const yp = a.y + (int64_t)first * a.y_stride + (int64_t)head * P;
+    const Rows brows = rows_at(a.b + (int64_t)first * a.b_stride + group * N, 1, N * e);
+    const Rows crows = rows_at(a.c + (int64_t)first * a.c_stride + group * N, 1, N * e);
+    const Rows xrows = rows_at(a.x + (int64_t)first * a.x_stride + (int64_t)head * P, 1, P * e);
+    const Rows zrows = rows_at(a.z + (int64_t)first * a.z_stride + (int64_t)head * P, a.z ? 1 : 0, P * e);
+    const Rows yrows = rows_at(a.y + (int64_t)first * a.y_stride + (int64_t)head * P, 1, P * e);
     float delta = (float)a.dt[(int64_t)first * a.dt_stride + head] + (a.dt_bias ? a.dt_bias[head] : 0.0f);
     Piece<T, V> b[CI], c[CI];
 #pragma unroll
     for (int i = 0; i < CI; ++i) {
         const int n = at_n + i * V * lpr;
-        b[i].template load<V == 4>(brows, n * (uint32_t)sizeof(T), N - n);
-        c[i].template load<V == 4>(crows, n * (uint32_t)sizeof(T), N - n);
+        b[i].template load<V == 4>(brows, n * e, N - n);
+        c[i].template load<V == 4>(crows, n * e, N - n);
     }
-    T x[U], z[U];
+    Piece<T, 1> x[U], z[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int p = min(p0 + u * rows, P - 1);
-        x[u] = xp[p];
-        z[u] = a.z ? zp[p] : (T)0.0f;
+        x[u].template load<false>(xrows, (p0 + u * rows) * e, 1);
+        z[u].template load<false>(zrows, (p0 + u * rows) * e, 1);
     }
     if (a.softplus) delta = softplus(delta);
     const float keep = expf(delta * a.a[head]), skip = a.d_skip ? a.d_skip[head] : 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int p = p0 + u * rows;
-        const float in_x = delta * (float)x[u];
+        const float in_x = delta * (float)x[u].v[0];
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < CI; ++i) {
-            const int n = at_n + i * V * lpr;
-            if (n < N) {
+            const bool has_n = at_n + i * V * lpr < N;              // (elsewhere infinities would meet zeros)
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    h[u][i][k] = keep * h[u][i][k] + in_x * (float)b[i].v[k];
-                    s = fmaf(h[u][i][k], (float)c[i].v[k], s);
-                }
-                if (leave && p < P) __builtin_nontemporal_store(h[u][i], (vec *)(out + (unsigned)(p * N + n)));
+            for (int k = 0; k < V; ++k) {
+                h[u][i][k] = keep * h[u][i][k] + in_x * (float)b[i].v[k];
+                s = has_n ? fmaf(h[u][i][k], (float)c[i].v[k], s) : s;
             }
+            if constexpr (V == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, h[u][i]), out, offset(u, i), 0, kStream);
+            else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, (float)h[u][i][0]), out, offset(u, i), 0, kStream);
         }
         for (int m = lpr >> 1; m > 0; m >>= 1) s += __shfl_xor(s, m);
-        if (p < P && at_n == 0) {
-            if (a.d_skip) s += skip * (float)x[u];
-            if (a.z) s *= silu_as<T>((float)z[u]);
-            yp[p] = (T)s;
-        }
+        if (a.d_skip) s += skip * (float)x[u].v[0];
+        if (a.z) s *= silu_as<T>((float)z[u].v[0]);
+        Piece<T, 1> y;
+        y.v[0] = (T)s;
+        y.template store<false>(yrows, (p0 + u * rows) * e, at_n == 0 ? 1 : 0);
     }
 }
 
