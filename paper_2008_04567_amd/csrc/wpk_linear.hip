@@ -434,17 +434,14 @@ linear_direct_kernel(LinearArgs a)
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
         from[i] = (uint32_t)((min(r0 + kLoadRows * i + load_row, last) - base) * (int)stride + piece(i)) * sizeof(T);
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)&lds[0][0] + wave * kLoads * 1024;
+    const uint32_t lds0 = lds_offset(&lds[0][0]) + wave * kLoads * 1024;
     auto fetch = [&](int stage, int k, int first, int end) {
         const uint32_t to = lds0 + stage * (uint32_t)sizeof(lds[0]);
         const bool whole = k + BK <= k_end;
 #pragma unroll
         for (int i = first; i < end; ++i) {
             const uint32_t off = whole || k + piece(i) < k_end ? from[i] : kOutside;      // (outside: zeros)
-            asm volatile("s_mov_b32 m0, %2\n s_nop 0\n buffer_load_dwordx4 %0, %1, %3 offen lds"
-                         :
-                         : "v"(off), "s"(src), "s"(to + i * 1024), "s"(k * (uint32_t)sizeof(T))
-                         : "memory");
+            load_to_lds(src, off, k * (uint32_t)sizeof(T), to + i * 1024);
         }
     };
     uint32_t read[BK / 16];                                    // where this lane's piece of a block's 16 entries is

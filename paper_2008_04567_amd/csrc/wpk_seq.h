@@ -172,6 +172,17 @@ template <typename T, int V> struct Piece {
     }
 };
 
+// 16 bytes a lane from `rows` at the lane's `offset` plus `step` straight to LDS, one lane's behind the other's from `lds`
+// on.  Not counted by the compiler: wait with s_waitcnt vmcnt before a barrier that lets anyone read them.
+__device__ inline uint32_t lds_offset(const void *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)p; }
+__device__ inline void load_to_lds(Rows rows, uint32_t offset, uint32_t step, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n s_nop 0\n buffer_load_dwordx4 %0, %1, %3 offen lds"
+                 :
+                 : "v"(offset), "s"(rows), "s"(lds), "s"(step)
+                 : "memory");
+}
+
 // ---- requests and their states (wpk.h, "sequence layers") ------------------------------------------------
 struct Requests {
     const int32_t *starts, *slot_map, *resume;

@@ -206,6 +206,41 @@ def test_scan_long_requests(S, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,head_dim,groups,state_dim", [(4, 64, 1, 128), (5, 64, 1, 72), (12, 40, 2, 64), (14, 8, 2, 8), (4, 128, 1, 32),
+                                                             (3, 136, 1, 40), (9, 24, 1, 120), (8, 200, 2, 16), (4, 64, 1, 130)])
+def test_scan_many_heads_a_group(S, dtype, heads, head_dim, groups, state_dim):
+    lengths = [0, 1, 2, 31, 33, 63, 64, 65, 130]
+    S.run_scan(lengths, heads, head_dim, groups, state_dim, dtype, resume=[1, 0, 1, 1, 0, 1, 0, 1, 1], in_place=True)
+    S.run_scan(lengths, heads, head_dim, groups, state_dim, dtype, gate=False, skip=False, bias=False, pad=8, offset=8)
+    S.run_scan([700, 3, 0, 1100], heads, head_dim, groups, state_dim, dtype, resume=[1, 1, 1, 0], in_place=True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_scan_many_heads_requests_values_and_alignment(S, dtype):
+    S.run_scan([900, 64], 4, 40, 1, 64, dtype, max_length=128, in_place=True)       # longer than the launch was shaped for
+    S.run_scan([4, 0, 70, 2], 6, 32, 1, 32, dtype, slot_map=[-1, 2, 99, 0])
+    S.run_scan([90, 600], 4, 64, 1, 64, dtype, state=False)
+    S.run_scan([70, 30], 4, 32, 1, 64, dtype, pad=4, offset=4)
+    S.run_scan([70, 30], 4, 32, 1, 64, dtype, pad=3, offset=1)
+    S.run_scan([40, 40, 40], 8, 32, 2, 32, dtype, uniform=True, in_place=True)
+
+    def edit(i):
+        i["x"][100, 5], i["x"][37, 70], i["x"][4, 250] = float("nan"), float("inf"), float("-inf")
+        i["z"][20, 2], i["c"][50, 7], i["b"][300, 3] = float("nan"), float("nan"), float("nan")
+        i["dt"][10::17] = 60.0
+    S.run_scan([130, 140, 70], 4, 64, 1, 128, dtype, edit=edit)
+
+
+def test_scan_many_requests_of_many_lengths(S):
+    # more workgroups than run at once: the longest first, in parts
+    r = np.random.default_rng(5)
+    lengths = [int(v) for v in r.integers(0, 90, 150)]
+    lengths[3], lengths[77], lengths[149] = 900, 0, 1500
+    S.run_scan(lengths, 8, 16, 1, 16, "bf16", resume=[i % 3 == 0 for i in range(150)])
+    S.run_scan(lengths, 8, 16, 1, 18, "bf16", in_place=True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("gate,skip,bias,softplus", [(False, False, False, True), (True, False, True, False), (False, True, False, False)])
 def test_scan_terms(S, dtype, gate, skip, bias, softplus):
     S.run_scan([70, 30], 4, 32, 2, 64, dtype, gate=gate, skip=skip, bias=bias, softplus=softplus)
