@@ -90,7 +90,7 @@ def build_library(force=True, verbose=False):
         headers + [src("wpk_igemm.h"), src("wpk_split.h"), src("wpk_strip.h"), src("wpk_strip_inst.hip")])
     for name in SEQUENCE_PARTS:
         add([hipcc] + COMMON + DEVICE + ["-c", src(name + ".hip"), "-o", os.path.join(OBJ, name + ".o")],
-            headers + [src("wpk_seq.h"), src("wpk_ssm_scan.h"), src("wpk_ssm_group.h"), src(name + ".hip")])
+            headers + [src("wpk_seq.h"), src("wpk_ssm_scan.h"), src(name + ".hip")])
     if jobs:
         workers = min(len(jobs), max(1, (os.cpu_count() or 4)), 16)
         with concurrent.futures.ThreadPoolExecutor(workers) as ex:

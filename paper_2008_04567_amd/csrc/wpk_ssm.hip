@@ -1,6 +1,6 @@
 // Selective state space scan: a state of head_dim x state_dim numbers per head, forgotten by exp(delta a) and fed by
 // delta x (outer) B at every token, read out by C.
-#include "wpk_ssm_group.h"
+#include "wpk_ssm_scan.h"
 
 namespace wpk {
 
@@ -117,39 +117,24 @@ static int scan_chunk(int dtype, int state_dim)     // tokens of a chunk (what f
 }
 
 struct ScanShape {
-    bool grouped;             // four heads of a group a workgroup (wpk_ssm_group.h), else one (wpk_ssm_scan.h)
     int n_parts, part_chunks;
     bool by_length;           // requests of different lengths that do not all start at once: the longest first
 };
 
-// Requests are cut along their tokens where their heads alone would leave compute units idle, or the longest request
-// would keep some at work when the rest are done.  Every part but a request's last is walked through twice, first for the state
-// that it leaves and then for y.
+// Requests are cut along their tokens where their heads alone would leave compute units idle.  Every part but a
+// request's last is walked through twice, first for the state that it leaves and then for y.
 static ScanShape scan_shape(const wpk_ssm_desc &d)
 {
-    const int q = scan_chunk(d.dtype, d.state_dim), blocks = (d.head_dim + 63) / 64;
-    ScanShape s = {false, 1, 1, false};
-    s.grouped = d.dtype == WPK_BF16 && d.state_dim <= 128 && d.state_dim % 8 == 0 && d.head_dim % 8 == 0 &&
-                d.heads / d.groups * blocks >= 4;
+    const int q = scan_chunk(d.dtype, d.state_dim);
     const int64_t chunks = ((int64_t)d.max_length + q - 1) / q;
-    s.part_chunks = (int)chunks;
-    if (d.sequences == 0) return s;
-    const int64_t teams = s.grouped ? (int64_t)d.groups * ((d.heads / d.groups * blocks + 3) / 4) : (int64_t)d.heads * blocks;
-    const int64_t room = (s.grouped ? 1 : 2) * kComputeUnits;      // workgroups that run at once
-    // chunks that each of them has to do, were they dealt out evenly
-    const int64_t all = d.tokens / q + (d.sequences + 1) / 2, share = (all * teams + room - 1) / room;
-    s.by_length = d.sequences > 1 && d.sequences <= 256 && teams * d.sequences > room;
-    if (chunks <= share || chunks < 8) return s;
-    int64_t each = d.sequences > 1 ? (share + 1) / 2 : share;
-    if (each < 4) each = 4;
-    int64_t most = (1ll << 30) / ((int64_t)d.sequences * d.heads * d.head_dim * d.state_dim * (int64_t)sizeof(float));   // 1 GiB of workspace
-    if (most > (s.grouped ? 32 : 16)) most = s.grouped ? 32 : 16;
-    if (most < 2) return s;
-    if ((chunks + each - 1) / each > most) each = (chunks + most - 1) / most;
-    s.n_parts = (int)((chunks + each - 1) / each);
-    s.part_chunks = (int)each;
-    if (s.n_parts < 2) s.n_parts = 1;
-    return s;
+    const int64_t groups = (int64_t)d.sequences * d.heads * ((d.head_dim + 63) / 64);
+    const int64_t room = 3 * kComputeUnits;
+    int64_t parts = groups > 0 ? room / groups : 1;
+    if (parts > 16) parts = 16;
+    if (parts > chunks / 4) parts = chunks / 4;
+    if (parts < 2) return {1, (int)chunks, groups > room && d.sequences > 1 && d.sequences <= 256};
+    const int64_t each = (chunks + parts - 1) / parts;
+    return {(int)((chunks + each - 1) / each), (int)each, false};
 }
 
 static size_t scan_part_bytes(const wpk_ssm_desc &d, const ScanShape &s)
@@ -179,32 +164,10 @@ template <typename T, int NPAD, int Q> static int launch_scan(const SsmArgs<T> &
     return a.vec_rows ? launch_scan_rows<T, NPAD, Q, true>(a, sequences, st) : launch_scan_rows<T, NPAD, Q, false>(a, sequences, st);
 }
 
-template <int NPAD> static int launch_group(const SsmArgs<bf16> &a, int sequences, hipStream_t st)
-{
-    const unsigned teams = a.groups * ((a.heads / a.groups * ((a.head_dim + 63) / 64) + 3) / 4);
-    if (a.n_parts > 1) {
-        hipLaunchKernelGGL((ssm_group_kernel<NPAD, false>), dim3(teams, a.n_parts - 1, sequences), dim3(512), 0, st, a);
-        WPK_HIP(hipGetLastError());
-        if (a.n_parts > 2) {
-            const dim3 grid((a.head_dim * a.state_dim + 1023) / 1024, a.heads, sequences);
-            hipLaunchKernelGGL((ssm_join_kernel<bf16, 64>), grid, dim3(256), 0, st, a);
-            WPK_HIP(hipGetLastError());
-        }
-    }
-    hipLaunchKernelGGL((ssm_group_kernel<NPAD, true>), dim3(teams, a.n_parts, sequences), dim3(512), 0, st, a);
-    WPK_HIP(hipGetLastError());
-    return WPK_OK;
-}
-
 template <typename T> struct ScanLaunch;
 template <> struct ScanLaunch<bf16> {
-    static int go(const SsmArgs<bf16> &a, bool grouped, int sequences, hipStream_t st)
+    static int go(const SsmArgs<bf16> &a, int sequences, hipStream_t st)
     {
-        if (grouped && a.vec_rows && a.vec_state) {
-            if (a.state_dim <= 32) return launch_group<32>(a, sequences, st);
-            if (a.state_dim <= 64) return launch_group<64>(a, sequences, st);
-            return launch_group<128>(a, sequences, st);
-        }
         if (a.state_dim <= 32) return launch_scan<bf16, 32, 64>(a, sequences, st);
         if (a.state_dim <= 64) return launch_scan<bf16, 64, 64>(a, sequences, st);
         if (a.state_dim <= 128) return launch_scan<bf16, 128, 64>(a, sequences, st);
@@ -212,7 +175,7 @@ template <> struct ScanLaunch<bf16> {
     }
 };
 template <> struct ScanLaunch<f16> {
-    static int go(const SsmArgs<f16> &a, bool, int sequences, hipStream_t st)
+    static int go(const SsmArgs<f16> &a, int sequences, hipStream_t st)
     {
         if (a.state_dim <= 32) return launch_scan<f16, 32, 64>(a, sequences, st);
         if (a.state_dim <= 64) return launch_scan<f16, 64, 64>(a, sequences, st);
@@ -221,7 +184,7 @@ template <> struct ScanLaunch<f16> {
     }
 };
 template <> struct ScanLaunch<float> {
-    static int go(const SsmArgs<float> &a, bool, int sequences, hipStream_t st)
+    static int go(const SsmArgs<float> &a, int sequences, hipStream_t st)
     {
         if (a.state_dim <= 32) return launch_scan<float, 32, 32>(a, sequences, st);
         if (a.state_dim <= 64) return launch_scan<float, 64, 32>(a, sequences, st);
@@ -261,15 +224,15 @@ static int ssm_typed(const wpk_ssm_desc &d, bool step, const void *x, const void
                        state_out, (T *)y, rq, d.heads, d.head_dim, d.groups, d.state_dim, d.dt_softplus,
                        d.x_stride, d.dt_stride, d.b_stride, d.c_stride, d.z_stride, d.y_stride,
                        nullptr, nullptr, shape.n_parts, shape.part_chunks, shape.by_length ? d.sequences : 0,
-                       d.state_dim % 8 == 0 && d.head_dim % 4 == 0 && rows_ok(b, d.b_stride, 8) && rows_ok(c, d.c_stride, 8) &&
-                           rows_ok(x, d.x_stride, shape.grouped ? 8 : 4) && (!z || rows_ok(z, d.z_stride, 4)) && rows_ok(y, d.y_stride, 4),
+                       d.state_dim % 8 == 0 && d.head_dim % 8 == 0 && rows_ok(b, d.b_stride, 8) && rows_ok(c, d.c_stride, 8) &&
+                           rows_ok(x, d.x_stride, 8) && (!z || rows_ok(z, d.z_stride, 4)) && rows_ok(y, d.y_stride, 4),
                        d.state_dim % 4 == 0 && aligned_to(state_in, 16) && aligned_to(state_out, 16)};
     if (step) return launch_step<T>(args, rows_ok(b, d.b_stride, 4) && rows_ok(c, d.c_stride, 4), d.sequences, st);
     if (shape.n_parts > 1) {
         args.parts = (float *)workspace;
         args.part_decay = (float *)((char *)workspace + scan_part_bytes(d, shape));
     }
-    return ScanLaunch<T>::go(args, shape.grouped, d.sequences, st);
+    return ScanLaunch<T>::go(args, d.sequences, st);
 }
 
 static int ssm_call(const wpk_ssm_desc *dp, bool step, const void *x, const void *dt, const float *a, const void *b,
