@@ -9,8 +9,16 @@
 // A workgroup of four waves walks through the chunks of one head (64 rows of its state, 16 a wave) with the state in
 // registers; nothing of it goes to memory between chunks.  All MFMAs are 16x16x32: the accumulators of h (column p in the
 // lane, rows n four by four) are, taken two blocks at a time, what the next product's operand wants with its reduction index
-// permuted, and C is read from LDS with the same permutation, so the state never crosses lanes either.  X stands in LDS
-// transposed and B both ways, transposed in registers on the way in.
+// permuted, and C is read from LDS with the same permutation, so the state never crosses lanes either.  B, C and X stand in
+// LDS as they come, once: what the other products want transposed is read by the transposing reads.  The order of a row's
+// 16-byte pieces depends on the row, so that neither kind of read meets a bank twice.  The next chunk's rows come into
+// registers while this one is worked on.
+//
+// Bound by issue: a chunk of 64 tokens by 128 state numbers costs a wave some 930 vector instructions (decays, splitting into
+// parts, offsets) beside 106 MFMAs, and what one wave of a SIMD spends the others cannot.  Hence two workgroups a compute
+// unit with all operands under way in registers: three, with rows fetched late, took 178 us instead of 170 (32 heads of 64 x
+// 128, 16384 tokens, bf16: 1.3 TB/s of x, z, b, c, y).  Four heads of a group in a workgroup, sharing G, took as long as one
+// by one; transposed copies of B and X in LDS, written on the way in, 168, and 259 instead of 247 for 24 ragged requests.
 //
 // Types.  Operands are taken as sums of bf16 numbers: one for bf16, two for fp16 (exact), three for fp32.  What is formed
 // in fp32 on the way keeps two of them (2^-17 of it) where y is rounded to 16 bits, and three (all 24 bits) for fp32 and
