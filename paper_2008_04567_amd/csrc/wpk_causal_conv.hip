@@ -158,7 +158,7 @@ static int conv_typed(const wpk_causal_conv_desc &d, const void *x, const void *
                       aligned_to(y, 16) && aligned_to(w, 16) && aligned_to(bias, 16) && aligned_to(state_in, 16) &&
                       aligned_to(state_out, 16);
     ConvArgs<T> a = {(const T *)x, (const T *)w, (const T *)bias, (const T *)state_in, (T *)state_out, (T *)y, rq,
-                     d.channels, wide ? d.channels / V : d.channels, (d.max_length + kRun - 1) / kRun, d.act,
+                     d.channels, wide ? d.channels / V : d.channels, (longest_request(d.tokens, d.max_length) + kRun - 1) / kRun, d.act,
                      d.x_stride, d.y_stride};
     // (a lane's number has 31 bits: a request of more runs than that is done by lanes that take several)
     const int64_t most = 0x40000000 / a.lanes;
@@ -176,7 +176,7 @@ static int conv_call(const wpk_causal_conv_desc *dp, bool step, const void *x, c
         d.x_stride < d.channels || d.y_stride < d.channels)
         return WPK_E_BAD_DESC;
     if (!seq_type_ok(d.dtype) || (d.act != WPK_ACT_NONE && d.act != WPK_ACT_SILU) || d.width > 8 ||
-        d.sequences > 65535 || d.channels > 0x3fffffff || d.x_stride >= (1ll << 40) || d.y_stride >= (1ll << 40))
+        d.sequences > 65535 || d.tokens > kMostRows || d.channels > 0x3fffffff || d.x_stride >= (1ll << 40) || d.y_stride >= (1ll << 40))
         return WPK_E_UNSUPPORTED;
     const size_t e = seq_type_bytes(d.dtype);
     int rc = check_requests(d.sequences, d.tokens, d.max_length, d.slots, step, starts, slot_map, resume, state_in, state_out, e);

@@ -558,7 +558,7 @@ static int check_linear(const wpk_linear_desc *dp)
     if (d.m < 0 || d.n < 1 || d.k < 1 || d.x_stride < d.k || d.w_stride < d.k || d.y_stride < d.n || d.residual_stride < d.n)
         return WPK_E_BAD_DESC;
     const int64_t most = 1ll << 20;
-    if (!seq_type_ok(d.dtype) || (d.y_dtype != d.dtype && d.y_dtype != WPK_F32) || d.act < WPK_ACT_NONE ||
+    if (d.m > kMostRows || d.n > kMostRows || !seq_type_ok(d.dtype) || (d.y_dtype != d.dtype && d.y_dtype != WPK_F32) || d.act < WPK_ACT_NONE ||
         d.act > WPK_ACT_GELU || d.x_stride >= most || d.w_stride >= most || d.y_stride >= most || d.residual_stride >= most)
         return WPK_E_UNSUPPORTED;
     return WPK_OK;

@@ -214,6 +214,14 @@ __device__ inline bool request_resumes(const Requests &q, int i)
     return !q.resume || __builtin_amdgcn_readfirstlane(q.resume[i]) != 0;
 }
 
+static const int32_t kMostRows = 1 << 30;      // of any matrix: row numbers of whole tiles and chunks stay below 2^31
+
+// tokens that the longest request can have, one at least: launches are shaped by max_length, which may be any upper bound
+inline int32_t longest_request(int32_t tokens, int32_t max_length)
+{
+    return max_length < tokens ? max_length : tokens > 0 ? tokens : 1;
+}
+
 // What the two kinds of call check alike; `step` for the calls of one token a request.
 inline int check_requests(int32_t sequences, int32_t tokens, int32_t max_length, int32_t slots, bool step, const void *starts,
                           const void *slot_map, const void *resume, const void *state_in, const void *state_out,

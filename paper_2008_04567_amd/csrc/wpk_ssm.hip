@@ -131,7 +131,7 @@ struct ScanShape {
 static ScanShape scan_shape(const wpk_ssm_desc &d)
 {
     const int q = scan_chunk(d.dtype, d.state_dim);
-    const int64_t chunks = ((int64_t)d.max_length + q - 1) / q;
+    const int64_t chunks = (longest_request(d.tokens, d.max_length) + q - 1) / q;
     const int64_t teams = (int64_t)d.heads * ((d.head_dim + 63) / 64), room = kResidents * kComputeUnits;
     ScanShape s = {1, (int)chunks, teams * d.sequences > room && d.sequences > 1 && d.sequences <= 256};
     if (d.sequences == 0) return s;
@@ -217,7 +217,7 @@ static int check_ssm(const wpk_ssm_desc *dp)
         return WPK_E_BAD_DESC;
     const int64_t most = 1ll << 22;
     if (!seq_type_ok(d.dtype) || d.dt_softplus < 0 || d.dt_softplus > 1 || d.head_dim > kMaxHeadDim ||
-        d.state_dim > kMaxStateDim || d.sequences > 65535 || d.heads > 65535 || d.x_stride >= most || d.dt_stride >= most ||
+        d.state_dim > kMaxStateDim || d.sequences > 65535 || d.tokens > kMostRows || d.heads > 65535 || d.x_stride >= most || d.dt_stride >= most ||
         d.b_stride >= most || d.c_stride >= most || d.z_stride >= most || d.y_stride >= most)
         return WPK_E_UNSUPPORTED;
     return WPK_OK;

@@ -328,6 +328,13 @@ def test_step_and_prompt_captured_in_a_graph(S):
         assert all(torch.equal(a, b) for a, b in zip(want, (y, o, out))), "replay %d" % turn
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_loose_bounds_on_lengths(S, dtype):
+    for bound in (1000, 2 ** 31 - 1):
+        S.run_conv([3, 90, 0, 1], 24, 4, dtype, max_length=bound, in_place=True)
+        S.run_scan([3, 700, 0, 1], 4, 16, 2, 40, dtype, max_length=bound, in_place=True)
+
+
 def test_offsets_beyond_32_bits(S):
     import torch
     B = S.B

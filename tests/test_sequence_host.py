@@ -146,3 +146,24 @@ def test_definitions_agree_with_closed_forms():
     y, _, _, _ = osq.ssm_scan(ones, np.ones((5, 1)), np.log(np.full(1, 0.5)), ones, ones, [(0, 5)], [np.full((1, 1, 1), 8.0)],
                               softplus=False)
     assert np.allclose(y[:, 0, 0], [5, 3.5, 2.75, 2.375, 2.1875])
+
+
+def test_more_rows_than_numbers_hold_are_refused():
+    most = 1 << 30
+    for change in (dict(m=most + 1), dict(n=most + 1)):
+        desc = B.make_linear_desc(**dict(LINEAR, **change))
+        assert status(B.linear_workspace, desc) == B.E_UNSUPPORTED
+        assert status(B.linear_fwd, desc, FAKE, FAKE, FAKE) == B.E_UNSUPPORTED
+    assert status(B.linear_workspace, B.make_linear_desc(**dict(LINEAR, m=most))) == B.OK
+    desc = B.make_causal_conv_desc(**dict(CONV, tokens=most + 1))
+    assert status(B.causal_conv1d_fwd, desc, FAKE, FAKE, FAKE, starts=FAKE) == B.E_UNSUPPORTED
+    desc = B.make_ssm_desc(**dict(SSM, tokens=most + 1))
+    assert status(B.ssm_workspace, desc) == B.E_UNSUPPORTED
+    assert status(B.ssm_scan_fwd, desc, *[FAKE] * 6, starts=FAKE, workspace=FAKE) == B.E_UNSUPPORTED
+
+
+def test_scan_workspace_follows_tokens_not_a_loose_bound_on_lengths():
+    def room(**change):
+        return B.ssm_workspace(B.make_ssm_desc(**dict(dict(SSM, sequences=2, tokens=4096, dtype=B.BF16), **change)))
+    assert room(max_length=2 ** 31 - 1) == room(max_length=4096)
+    assert room(max_length=2 ** 31 - 1, tokens=0) == 0
