@@ -535,7 +535,7 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
 };
 
 // workgroups that share a compute unit, by LDS; rows that are moved element by element take more registers
-template <typename Scan, bool WIDE> constexpr int scan_residents() { return sizeof(typename Scan::Shared) > 81920 ? 1 : sizeof(typename Scan::Shared) > 48000 || !WIDE ? 2 : 3; }
+template <typename Scan, bool WIDE> constexpr int scan_residents() { return sizeof(typename Scan::Shared) > 81920 ? 1 : sizeof(typename Scan::Shared) > 42000 || !WIDE ? 2 : 3; }
 
 template <typename T, int NPAD, int Q, bool FULL, bool WIDE>
 __global__ void __launch_bounds__(256, (scan_residents<SsmScan<T, NPAD, Q, FULL, WIDE>, WIDE>()))
