@@ -111,15 +111,10 @@ template <typename T> static int launch_step(const SsmArgs<T> &a, bool vec_bc, i
 }
 
 // ---- prompts -----------------------------------------------------------------------------------------------
-static int scan_chunk(int dtype, int state_dim)     // tokens of a chunk (what fits LDS)
-{
-    if (dtype == WPK_BF16) return 64;
-    return dtype == WPK_F16 && state_dim <= 128 ? 64 : 32;
-}
-
 static const int kResidents = 2;      // workgroups that share a compute unit (most types and sizes)
+static const int kPartUnit = 64;      // tokens that parts are multiples of: whole chunks of every kernel
 struct ScanShape {
-    int n_parts, part_chunks;
+    int n_parts, part_units;
     bool by_length;           // requests of different lengths that do not all start at once: the longest first
 };
 
@@ -130,22 +125,21 @@ struct ScanShape {
 // whole, the longest first, and 247 in up to three parts.
 static ScanShape scan_shape(const wpk_ssm_desc &d)
 {
-    const int q = scan_chunk(d.dtype, d.state_dim);
-    const int64_t chunks = (longest_request(d.tokens, d.max_length) + q - 1) / q;
+    const int64_t units = (longest_request(d.tokens, d.max_length) + kPartUnit - 1) / kPartUnit;
     const int64_t teams = (int64_t)d.heads * ((d.head_dim + 63) / 64), room = kResidents * kComputeUnits;
-    ScanShape s = {1, (int)chunks, teams * d.sequences > room && d.sequences > 1 && d.sequences <= 256};
+    ScanShape s = {1, (int)units, teams * d.sequences > room && d.sequences > 1 && d.sequences <= 256};
     if (d.sequences == 0) return s;
-    // chunks for each workgroup that runs at once, were they dealt out evenly
-    const int64_t all = d.tokens / q + (d.sequences + 1) / 2, share = (all * teams + room - 1) / room;
-    if (chunks < 8 || chunks <= 2 * share) return s;
+    // units for each workgroup that runs at once, were they dealt out evenly
+    const int64_t all = d.tokens / kPartUnit + (d.sequences + 1) / 2, share = (all * teams + room - 1) / room;
+    if (units < 8 || units <= 2 * share) return s;
     int64_t each = share < 4 ? 4 : share;
     // (at most a GiB of workspace)
     int64_t most = (1ll << 30) / ((int64_t)d.sequences * d.heads * d.head_dim * d.state_dim * (int64_t)sizeof(float));
     if (most > 32) most = 32;
     if (most < 2) return s;
-    if ((chunks + each - 1) / each > most) each = (chunks + most - 1) / most;
-    s.n_parts = (int)((chunks + each - 1) / each);
-    s.part_chunks = (int)each;
+    if ((units + each - 1) / each > most) each = (units + most - 1) / most;
+    s.n_parts = (int)((units + each - 1) / each);
+    s.part_units = (int)each;
     return s;
 }
 
@@ -154,8 +148,9 @@ static size_t scan_part_bytes(const wpk_ssm_desc &d, const ScanShape &s)
     return (size_t)d.sequences * d.heads * s.n_parts * d.head_dim * d.state_dim * sizeof(float);
 }
 
-template <typename T, int NPAD, int Q, bool WIDE> static int launch_scan_rows(const SsmArgs<T> &a, int sequences, hipStream_t st)
+template <typename T, int NPAD, int Q, bool WIDE> static int launch_scan_rows(SsmArgs<T> a, int sequences, hipStream_t st)
 {
+    a.part_chunks *= kPartUnit / Q;
     const unsigned heads = a.heads * ((a.head_dim + 63) / 64);
     if (a.n_parts > 1) {
         hipLaunchKernelGGL((ssm_scan_kernel<T, NPAD, Q, false, WIDE>), dim3(heads, a.n_parts - 1, sequences), dim3(256), 0, st, a);
@@ -171,39 +166,29 @@ template <typename T, int NPAD, int Q, bool WIDE> static int launch_scan_rows(co
     return WPK_OK;
 }
 
-template <typename T, int NPAD, int Q> static int launch_scan(const SsmArgs<T> &a, int sequences, hipStream_t st)
+// Chunks of 64 tokens where two workgroups of them fit a compute unit, else of 32: 32 heads of 64 numbers, 16384 tokens,
+// bf16, states of 128: 151 us by 64 and 168 by 32; of 256: 288 and 387; f16, of 64: 155 and 173; of 128: 273 and 233.  But a
+// workgroup that has its compute unit to itself gains nothing by smaller ones: f16, 10 heads of 48 x 72, 9 requests of 1001
+// tokens together, 32 us by 64 and 40 by 32.  Rows that are moved element by element take more registers: bf16, of 128: 535
+// and 338; of 256: 1025 and 820.
+template <typename T, int NPAD> static int launch_scan(const SsmArgs<T> &a, int sequences, hipStream_t st)
 {
-    return a.vec_rows ? launch_scan_rows<T, NPAD, Q, true>(a, sequences, st) : launch_scan_rows<T, NPAD, Q, false>(a, sequences, st);
+    const int Q = sizeof(T) == 4 || (SsmType<T>::parts == 2 && NPAD > 64) ? 32 : 64;
+    if (!a.vec_rows) return launch_scan_rows<T, NPAD, 32, false>(a, sequences, st);
+    if constexpr (SsmType<T>::parts == 2 && NPAD == 128) {
+        const int64_t workgroups = (int64_t)sequences * a.heads * ((a.head_dim + 63) / 64) * a.n_parts;
+        if (workgroups <= kComputeUnits) return launch_scan_rows<T, NPAD, 64, true>(a, sequences, st);
+    }
+    return launch_scan_rows<T, NPAD, Q, true>(a, sequences, st);
 }
 
-template <typename T> struct ScanLaunch;
-template <> struct ScanLaunch<bf16> {
-    static int go(const SsmArgs<bf16> &a, int sequences, hipStream_t st)
-    {
-        if (a.state_dim <= 32) return launch_scan<bf16, 32, 64>(a, sequences, st);
-        if (a.state_dim <= 64) return launch_scan<bf16, 64, 64>(a, sequences, st);
-        if (a.state_dim <= 128) return launch_scan<bf16, 128, 64>(a, sequences, st);
-        return launch_scan<bf16, 256, 64>(a, sequences, st);
-    }
-};
-template <> struct ScanLaunch<f16> {
-    static int go(const SsmArgs<f16> &a, int sequences, hipStream_t st)
-    {
-        if (a.state_dim <= 32) return launch_scan<f16, 32, 64>(a, sequences, st);
-        if (a.state_dim <= 64) return launch_scan<f16, 64, 64>(a, sequences, st);
-        if (a.state_dim <= 128) return launch_scan<f16, 128, 64>(a, sequences, st);
-        return launch_scan<f16, 256, 32>(a, sequences, st);
-    }
-};
-template <> struct ScanLaunch<float> {
-    static int go(const SsmArgs<float> &a, int sequences, hipStream_t st)
-    {
-        if (a.state_dim <= 32) return launch_scan<float, 32, 32>(a, sequences, st);
-        if (a.state_dim <= 64) return launch_scan<float, 64, 32>(a, sequences, st);
-        if (a.state_dim <= 128) return launch_scan<float, 128, 32>(a, sequences, st);
-        return launch_scan<float, 256, 32>(a, sequences, st);
-    }
-};
+template <typename T> static int launch_scan(const SsmArgs<T> &a, int sequences, hipStream_t st)
+{
+    if (a.state_dim <= 32) return launch_scan<T, 32>(a, sequences, st);
+    if (a.state_dim <= 64) return launch_scan<T, 64>(a, sequences, st);
+    if (a.state_dim <= 128) return launch_scan<T, 128>(a, sequences, st);
+    return launch_scan<T, 256>(a, sequences, st);
+}
 
 static int check_ssm(const wpk_ssm_desc *dp)
 {
@@ -235,7 +220,7 @@ static int ssm_typed(const wpk_ssm_desc &d, bool step, const void *x, const void
     SsmArgs<T> args = {(const T *)x, (const T *)dt, (const T *)b, (const T *)c, (const T *)z, a, d_skip, dt_bias, state_in,
                        state_out, (T *)y, rq, d.heads, d.head_dim, d.groups, d.state_dim, d.dt_softplus,
                        d.x_stride, d.dt_stride, d.b_stride, d.c_stride, d.z_stride, d.y_stride,
-                       nullptr, nullptr, shape.n_parts, shape.part_chunks, shape.by_length ? d.sequences : 0,
+                       nullptr, nullptr, shape.n_parts, shape.part_units, shape.by_length ? d.sequences : 0,
                        d.state_dim % 8 == 0 && d.head_dim % 8 == 0 && rows_ok(b, d.b_stride, 8) && rows_ok(c, d.c_stride, 8) &&
                            rows_ok(x, d.x_stride, 8) && (!z || rows_ok(z, d.z_stride, 4)) && rows_ok(y, d.y_stride, 4),
                        d.state_dim % 4 == 0 && aligned_to(state_in, 16) && aligned_to(state_out, 16)};
@@ -244,7 +229,7 @@ static int ssm_typed(const wpk_ssm_desc &d, bool step, const void *x, const void
         args.parts = (float *)workspace;
         args.part_decay = (float *)((char *)workspace + scan_part_bytes(d, shape));
     }
-    return ScanLaunch<T>::go(args, d.sequences, st);
+    return launch_scan<T>(args, d.sequences, st);
 }
 
 static int ssm_call(const wpk_ssm_desc *dp, bool step, const void *x, const void *dt, const float *a, const void *b,

@@ -43,7 +43,7 @@ template <typename T> struct SsmArgs {
     float *parts;             // workspace: [request][head][parts][head_dim][state_dim], then [request][head][parts] decays
     float *part_decay;
     int32_t n_parts;          // parts that a request may have
-    int32_t part_chunks;      // chunks of a part (the last one takes what is left)
+    int32_t part_chunks;      // chunks of a part (the last one takes what is left); before the launch: units of 64 tokens
     int32_t sequences;        // 0 where requests are done in their order, else as many, the longest first (256 at most)
     int32_t vec_rows, vec_state;   // whether rows (of the tensors, of the states) start at multiples of 16 bytes
 };

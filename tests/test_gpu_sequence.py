@@ -329,6 +329,13 @@ def test_step_and_prompt_captured_in_a_graph(S):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_scan_more_workgroups_than_compute_units(S, dtype):
+    for pad in (0, 1):                                     # rows at multiples of 16 bytes, and not
+        S.run_scan([70, 200, 31], 160, 16, 2, 96, dtype, pad=pad, in_place=True)
+        S.run_scan([33, 600], 4, 16, 1, 96, dtype, pad=pad)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_loose_bounds_on_lengths(S, dtype):
     for bound in (1000, 2 ** 31 - 1):
         S.run_conv([3, 90, 0, 1], 24, 4, dtype, max_length=bound, in_place=True)
