@@ -14,11 +14,13 @@
 // 16-byte pieces depends on the row, so that neither kind of read meets a bank twice.  The next chunk's rows come into
 // registers while this one is worked on.
 //
-// Bound by issue: a chunk of 64 tokens by 128 state numbers costs a wave some 930 vector instructions (decays, splitting into
-// parts, offsets) beside 106 MFMAs, and what one wave of a SIMD spends the others cannot.  Hence two workgroups a compute
-// unit with all operands under way in registers: three, with rows fetched late, took 178 us instead of 170 (32 heads of 64 x
-// 128, 16384 tokens, bf16: 1.3 TB/s of x, z, b, c, y).  Four heads of a group in a workgroup, sharing G, took as long as one
-// by one; transposed copies of B and X in LDS, written on the way in, 168, and 259 instead of 247 for 24 ragged requests.
+// Bound by issue and by what waits on it: a chunk of 64 tokens by 128 state numbers costs a wave some 930 vector instructions
+// (decays, splitting into parts, offsets) beside 106 MFMAs, and what one wave of a SIMD spends the others cannot.  16384 tokens
+// of 32 heads of 64 x 128 numbers, bf16: 118 us for this pass (vector units 49 % busy, matrix pipes 20 %, LDS conflicts 11 %
+// of its time, 1.9 TB/s), 46 for the one that leaves the parts' states.  Two workgroups a compute unit with all operands under
+// way in registers: three, with rows fetched late, took 178 us in all instead of 170.  Four heads of a group in a workgroup,
+// sharing G, took as long as one by one; a wave that forms the next chunk's decays beside the others' products 175; transposed
+// copies of B and X in LDS, written on the way in, 168, and 259 instead of 247 for 24 ragged requests.
 //
 // Types.  Operands are taken as sums of bf16 numbers: one for bf16, two for fp16 (exact), three for fp32.  What is formed
 // in fp32 on the way keeps two of them (2^-17 of it) where y is rounded to 16 bits, and three (all 24 bits) for fp32 and
@@ -96,10 +98,13 @@ template <int PARTS, typename T> __device__ inline void parts_of(T v, bf16 (&out
     }
 }
 
-// What is xored to the number of a 16-byte piece in a row of NCH pieces; the same for rows 32 apart.
+// What is xored to the number of a 16-byte piece in a row of NCH pieces; the same for rows 16 apart.  Reads of one piece of 16
+// rows meet every bank once, and so do transposing reads, whose half a wave takes 32 bytes (two pieces) of rows r .. r + 3
+// and r + 8 .. r + 11, r a multiple of four.
 template <int NCH> __device__ inline int piece_order(int row)
 {
-    return NCH >= 16 ? (row & 15) ^ ((row >> 4) & 1) << 2 : NCH == 8 ? ((row >> 1) & 7) ^ ((row >> 4) & 1) << 1 : (row >> 2) & 3;
+    const int pair = NCH >= 16 ? (row & 3) | (row >> 1 & 4) : NCH == 8 ? (row >> 1 & 1) | (row >> 2 & 2) : row >> 3 & 1;
+    return pair << 1 | (row >> 2 & 1);
 }
 template <int NCH> __device__ inline int piece_at(int row, int piece) { return (row * NCH + (piece ^ piece_order<NCH>(row))) * 8; }
 
@@ -316,7 +321,6 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
 #pragma unroll
             for (int q = 0; q < YP; ++q) *(bf16x4 *)&sm.m[FULL ? q : 0][m_at(t, s0)] = w;
         }
-        const int kNext = 8 * (NCH >= 16 ? 4 : NCH == 8 ? 2 : 1), kOdd = 8 * (NCH >= 16 ? 4 : NCH == 8 ? 2 : 0);
 
         float total = 1.0f;
         if (c0 < c1) {
@@ -334,8 +338,8 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
             asm volatile("" : "+v"(lane_col), "+v"(lane_g));
             const int col = lane_col, g = lane_g;
             // Where this lane's first pieces are: of four rows for the transposing reads of B (blocks of 16 columns) and X, of
-            // rows t of C.  Other pieces of a row are at that xor 8 times theirs; rows 4 on (a second transposing read) and 16
-            // on (C's odd blocks) differ from it by one bit of the order.
+            // rows t of C.  Other pieces of a row are at that xor 8 times theirs, and in rows 4 on (a second
+            // transposing read) at that xor 8.
             const int trow = 8 * g + (col >> 2), half4 = (col & 1) * 4;
             const int at_b = piece_at<NCH>(trow, (col >> 1) & 1) + half4, at_c = piece_at<NCH>(col, g >> 1) + 4 * (g & 1);
             const int at_x = piece_at<8>(trow, 2 * wave + ((col >> 1) & 1)) + half4;
@@ -399,7 +403,7 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
                     split(__builtin_shufflevector(h[2 * n], h[2 * n + 1], 0, 1, 2, 3, 4, 5, 6, 7), fh);
 #pragma unroll
                     for (int i = 0; i < QB; ++i) {
-                        const int at = at_c ^ 32 * n ^ (i & 1 ? kOdd : 0);
+                        const int at = at_c ^ 32 * n;
 #pragma unroll
                         for (int q = 0; q < NP; ++q) {
                             const bf16 *const rows = &sm.c[q][16 * i * NPAD];
@@ -434,7 +438,7 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
 #pragma unroll
                 for (int q = 0; q < NP; ++q) {
                     const bf16x4 lo = read_transposed(&sm.x[q][32 * k * 64 + at_x]);
-                    const bf16x4 hi = read_transposed(&sm.x[q][(32 * k + 4) * 64 + (at_x ^ 16)]);
+                    const bf16x4 hi = read_transposed(&sm.x[q][(32 * k + 4) * 64 + (at_x ^ 8)]);
                     fx[k][q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                 }
             // Infinities or NaN among x may not meet the zeros of M that stand for later tokens: x times zero finds them.
@@ -464,7 +468,7 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
                         for (int q = 0; q < NP; ++q) {
                             const int at = at_b ^ 16 * (i0 + i);
                             const bf16x4 lo = read_transposed(&sm.b[q][32 * k * NPAD + at]);
-                            const bf16x4 hi = read_transposed(&sm.b[q][(32 * k + 4) * NPAD + (at ^ kNext)]);
+                            const bf16x4 hi = read_transposed(&sm.b[q][(32 * k + 4) * NPAD + (at ^ 8)]);
                             fb[i][q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                         }
                     each_pair<3, NP, 3>([&](int u, int v) {
