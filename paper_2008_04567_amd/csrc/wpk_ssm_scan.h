@@ -1,4 +1,4 @@
-// Selective state space scan over prompts, in chunks of kQ tokens on the bf16 matrix pipes.
+// Selective state space scan over prompts, in chunks of Q tokens on the bf16 matrix pipes.
 //
 // With S the running sum of delta a within a chunk, h0 the state before it and G = C B^T:
 //   M[t][s] = G[t][s] exp(S_t - S_s) delta_s  (s <= t; d on the diagonal too)     y = M X + exp(S_t) C h0
@@ -11,13 +11,13 @@
 // lane, rows n four by four) are, taken two blocks at a time, what the next product's operand wants with its reduction index
 // permuted, and C is read from LDS with the same permutation, so the state never crosses lanes either.  B, C and X stand in
 // LDS as they come, once: what the other products want transposed is read by the transposing reads.  The order of a row's
-// 16-byte pieces depends on the row, so that neither kind of read meets a bank twice.  The next chunk's rows come into
+// 16-byte pieces depends on the row, so that neither whole pieces nor transposing reads meet a bank twice.  The next chunk's rows come into
 // registers while this one is worked on.
 //
 // Bound by issue and by what waits on it: a chunk of 64 tokens by 128 state numbers costs a wave some 930 vector instructions
 // (decays, splitting into parts, offsets) beside 106 MFMAs, and what one wave of a SIMD spends the others cannot.  16384 tokens
 // of 32 heads of 64 x 128 numbers, bf16: 118 us for this pass (vector units 49 % busy, matrix pipes 20 %, LDS conflicts 11 %
-// of its time, 1.9 TB/s), 46 for the one that leaves the parts' states.  Two workgroups a compute unit with all operands under
+// of its time, from C's reads, which the compiler joins two rows apart by 16 to one: 1.8 TB/s), 46 for the one that leaves the parts' states.  Two workgroups a compute unit with all operands under
 // way in registers: three, with rows fetched late, took 178 us in all instead of 170.  Four heads of a group in a workgroup,
 // sharing G, took as long as one by one; a wave that forms the next chunk's decays beside the others' products 175; transposed
 // copies of B and X in LDS, written on the way in, 168, and 259 instead of 247 for 24 ragged requests.
