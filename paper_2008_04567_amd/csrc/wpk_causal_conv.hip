@@ -1,7 +1,7 @@
 // Short causal convolution of every channel by itself, over ragged requests that carry a state.
 //
 // y[t][c] = act(bias[c] + sum_j w[c][j] x[t - (W-1) + j][c]).  Bound by memory: every value is read once and written
-// once for W multiply-adds.  A lane owns V channels (16 bytes where rows are aligned) and a run of kRun tokens: it
+// once for W multiply-adds.  A lane owns V channels (16 bytes where rows start at multiples of four) and a run of kRun tokens: it
 // keeps the last W - 1 rows in registers, so rows are read W - 1 times more than once per run only, and asks for kAhead
 // rows at once.  16384 ragged tokens of 4352 bf16 channels: 62 us, 4.6 TB/s (before its weights were read by vectors, 66; so
 // measured, runs of 16 took 67, four rows at once 72, two 80).
@@ -13,7 +13,7 @@ static const int kRun = 32;   // tokens of a run
 static const int kAhead = 8;  // rows under way
 
 template <typename T, int V> struct Row {
-    typedef T vec __attribute__((ext_vector_type(V)));
+    typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));      // (the device takes such loads and stores)
 };
 
 template <typename T, int V> __device__ inline void load_row(const T *p, float (&out)[V])
@@ -23,12 +23,16 @@ template <typename T, int V> __device__ inline void load_row(const T *p, float (
     for (int i = 0; i < V; ++i) out[i] = (float)a[i];
 }
 
-template <typename T, int V> __device__ inline void store_row(T *p, const float (&in)[V])
+// but for the first `skip`
+template <typename T, int V> __device__ inline void store_row(T *p, typename Row<T, V>::vec v, int skip)
 {
-    typename Row<T, V>::vec a;
+    if (skip == 0) {
+        *(typename Row<T, V>::vec *)p = v;
+    } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) a[i] = (T)in[i];
-    *(typename Row<T, V>::vec *)p = a;
+        for (int i = 0; i < V; ++i)
+            if (i >= skip) p[i] = v[i];
+    }
 }
 
 template <typename T> struct ConvArgs {
@@ -40,13 +44,14 @@ template <typename T> struct ConvArgs {
 };
 
 // Grid: (lanes of all runs / 256, requests).  Rows before a request's first come from its state; the lane of the first
-// run also writes the state that the request leaves, after it has read the old one, so the two may be the same.
+// run also writes the state that the request leaves, after it has read the old one, so the two may be the same.  The last
+// lane of a row takes the row's last V channels and stores those that no lane before it has.
 template <typename T, int V, int W> __global__ void __launch_bounds__(256) causal_conv_kernel(ConvArgs<T> a)
 {
     const int lane = blockIdx.x * 256 + threadIdx.x;
     int run = lane / a.lanes;
     if (run >= a.runs) return;
-    const int c = (lane - run * a.lanes) * V;
+    const int c_first = (lane - run * a.lanes) * V, c = min(c_first, a.channels - V), skip = c_first - c;
     int first, length;
     request_rows(a.rq, blockIdx.y, &first, &length);
     const bool head = run == 0;
@@ -81,6 +86,7 @@ template <typename T, int V, int W> __global__ void __launch_bounds__(256) causa
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) {      // row j of the new state is row length + j of [old state | x]
                 float r[V];
+                typename Row<T, V>::vec left;
                 const int row = length - (W - 1) + j;
                 if (row >= 0) load_row<T, V>(x + (int64_t)row * a.x_stride, r);
                 else {
@@ -92,7 +98,9 @@ template <typename T, int V, int W> __global__ void __launch_bounds__(256) causa
 #pragma unroll
                             for (int i = 0; i < V; ++i) r[i] = win[o][i];
                 }
-                store_row<T, V>(a.state_out + at + (size_t)j * a.channels, r);
+#pragma unroll
+                for (int i = 0; i < V; ++i) left[i] = (T)r[i];
+                store_row<T, V>(a.state_out + at + (size_t)j * a.channels, left, skip);
             }
         }
     }
@@ -121,7 +129,7 @@ template <typename T, int V, int W> __global__ void __launch_bounds__(256) causa
 #pragma unroll
                     for (int j = 0; j < W - 1; ++j) win[j][i] = win[j + 1][i];
                 }
-                if (t + u < t1) *(typename Row<T, V>::vec *)(y + (int64_t)(t + u) * a.y_stride) = out;
+                if (t + u < t1) store_row<T, V>(y + (int64_t)(t + u) * a.y_stride, out, skip);
             }
         }
     }
@@ -152,14 +160,16 @@ template <typename T>
 static int conv_typed(const wpk_causal_conv_desc &d, const void *x, const void *w, const void *bias, const Requests &rq,
                       const void *state_in, void *state_out, void *y, hipStream_t st)
 {
-    // 16 bytes of channels a lane where every row starts at a multiple of 16 bytes, else one channel
+    // 16 bytes of channels a lane where every row starts at a multiple of four, else one channel: 16384 tokens of 4348 bf16
+    // channels take 72 us by 16 bytes and 90 by one; rows at odd multiples of two gain in large calls only (4351 channels: 76
+    // and 90) and lose in others (2000 tokens of 1763: 17.7 and 9.6)
     const int V = 16 / (int)sizeof(T);
-    const bool wide = d.channels % V == 0 && d.x_stride % V == 0 && d.y_stride % V == 0 && aligned_to(x, 16) &&
-                      aligned_to(y, 16) && aligned_to(w, 16) && aligned_to(bias, 16) && aligned_to(state_in, 16) &&
-                      aligned_to(state_out, 16);
+    auto fours = [](const void *p, int64_t stride) { return aligned_to(p, 4) && stride * (int64_t)sizeof(T) % 4 == 0; };
+    const bool wide = d.channels >= V && fours(x, d.x_stride) && fours(y, d.y_stride) && fours(w, 0) && fours(bias, 0) &&
+                      fours(state_in, d.channels) && fours(state_out, d.channels);
     ConvArgs<T> a = {(const T *)x, (const T *)w, (const T *)bias, (const T *)state_in, (T *)state_out, (T *)y, rq,
-                     d.channels, wide ? d.channels / V : d.channels, (longest_request(d.tokens, d.max_length) + kRun - 1) / kRun, d.act,
-                     d.x_stride, d.y_stride};
+                     d.channels, wide ? (d.channels + V - 1) / V : d.channels,
+                     (longest_request(d.tokens, d.max_length) + kRun - 1) / kRun, d.act, d.x_stride, d.y_stride};
     // (a lane's number has 31 bits: a request of more runs than that is done by lanes that take several)
     const int64_t most = 0x40000000 / a.lanes;
     if (a.runs > most) a.runs = (int32_t)(most < 1 ? 1 : most);

@@ -148,6 +148,14 @@ def test_conv_strides_and_alignment(S, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("channels", [4, 6, 9, 10, 42, 70, 2054])
+def test_conv_channels_that_fill_no_lane(S, dtype, channels):
+    lengths = [0, 1, 2, 33, 100]
+    S.run_conv(lengths, channels, 4, dtype, resume=[1, 0, 1, 0, 1], in_place=True)
+    S.run_conv(lengths, channels, 3, dtype, pad=(2, 6), offset=2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_conv_requests(S, dtype):
     S.run_conv([20, 20, 20], 24, 4, dtype, uniform=True, in_place=True)
     S.run_conv([3, 90, 5], 24, 4, dtype, max_length=16, in_place=True)          # longer than the launch was shaped for
