@@ -213,18 +213,18 @@ static int ssm_typed(const wpk_ssm_desc &d, bool step, const void *x, const void
                      const float *d_skip, const void *z, const float *dt_bias, const Requests &rq, const float *state_in,
                      float *state_out, void *y, void *workspace, hipStream_t st)
 {
-    const size_t e = sizeof(T);
-    auto rows_ok = [&](const void *p, int64_t stride, int v) { return stride % v == 0 && aligned_to(p, v * e < 16 ? v * e : 16); };
+    // buffer accesses of up to 16 bytes want multiples of four
+    auto rows_ok = [&](const void *p, int64_t stride) { return stride * (int64_t)sizeof(T) % 4 == 0 && aligned_to(p, 4); };
     ScanShape shape = scan_shape(d);
     if (!rq.starts) shape.by_length = false;
     SsmArgs<T> args = {(const T *)x, (const T *)dt, (const T *)b, (const T *)c, (const T *)z, a, d_skip, dt_bias, state_in,
                        state_out, (T *)y, rq, d.heads, d.head_dim, d.groups, d.state_dim, d.dt_softplus,
                        d.x_stride, d.dt_stride, d.b_stride, d.c_stride, d.z_stride, d.y_stride,
                        nullptr, nullptr, shape.n_parts, shape.part_units, shape.by_length ? d.sequences : 0,
-                       d.state_dim % 8 == 0 && d.head_dim % 8 == 0 && rows_ok(b, d.b_stride, 8) && rows_ok(c, d.c_stride, 8) &&
-                           rows_ok(x, d.x_stride, 8) && (!z || rows_ok(z, d.z_stride, 4)) && rows_ok(y, d.y_stride, 4),
+                       d.state_dim % 8 == 0 && d.head_dim % 8 == 0 && rows_ok(b, d.b_stride) && rows_ok(c, d.c_stride) &&
+                           rows_ok(x, d.x_stride) && (!z || rows_ok(z, d.z_stride)) && rows_ok(y, d.y_stride),
                        d.state_dim % 4 == 0 && aligned_to(state_in, 16) && aligned_to(state_out, 16)};
-    if (step) return launch_step<T>(args, rows_ok(b, d.b_stride, 4) && rows_ok(c, d.c_stride, 4), d.sequences, st);
+    if (step) return launch_step<T>(args, rows_ok(b, d.b_stride) && rows_ok(c, d.c_stride), d.sequences, st);
     if (shape.n_parts > 1) {
         args.parts = (float *)workspace;
         args.part_decay = (float *)((char *)workspace + scan_part_bytes(d, shape));

@@ -47,7 +47,9 @@ template <typename T> struct SsmArgs {
     int32_t n_parts;          // parts that a request may have
     int32_t part_chunks;      // chunks of a part (the last one takes what is left); before the launch: units of 64 tokens
     int32_t sequences;        // 0 where requests are done in their order, else as many, the longest first (256 at most)
-    int32_t vec_rows, vec_state;   // whether rows (of the tensors, of the states) start at multiples of 16 bytes
+    // whether rows of the tensors start at multiples of four bytes and hold whole groups of eight; of the states, at multiples of
+    // 16 bytes
+    int32_t vec_rows, vec_state;
 };
 
 template <typename T> struct SsmType;

@@ -337,8 +337,16 @@ def test_step_and_prompt_captured_in_a_graph(S):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("state_dim", [16, 56, 128, 200])
+def test_scan_rows_at_multiples_of_four_bytes(S, dtype, state_dim):
+    for heads, head_dim, pad, offset in ((3, 24, 2, 2), (6, 72, 6, 0), (1, 8, 2, 4)):
+        S.run_scan([1, 90, 0, 200], heads, head_dim, 1, state_dim, dtype, pad=pad, offset=offset, resume=[1, 0, 1, 1])
+        S.run_scan([1] * 5, heads, head_dim, 1, state_dim, dtype, pad=pad, offset=offset, step=True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_scan_more_workgroups_than_compute_units(S, dtype):
-    for pad in (0, 1):                                     # rows at multiples of 16 bytes, and not
+    for pad in (0, 2, 1):                                  # rows at multiples of 16 bytes, of four and of two
         S.run_scan([70, 200, 31], 160, 16, 2, 96, dtype, pad=pad, in_place=True)
         S.run_scan([33, 600], 4, 16, 1, 96, dtype, pad=pad)
 
