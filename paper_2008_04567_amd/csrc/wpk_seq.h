@@ -180,7 +180,7 @@ __device__ inline void load_to_lds(Rows rows, uint32_t offset, uint32_t step, ui
     asm volatile("s_mov_b32 m0, %2\n s_nop 0\n buffer_load_dwordx4 %0, %1, %3 offen lds"
                  :
                  : "v"(offset), "s"(rows), "s"(lds), "s"(step)
-                 : "memory");
+                 : "m0", "memory");
 }
 
 // ---- requests and their states (wpk.h, "sequence layers") ------------------------------------------------
