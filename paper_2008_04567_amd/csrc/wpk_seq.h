@@ -46,10 +46,13 @@ template <typename T> __device__ inline float silu_as(float v) { return sizeof(T
 __device__ inline float softplus(float v) { return fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v))); }
 
 // log(1 + e) as log(u) e / (u - 1) with u = 1 + e rounded (Goldberg 1991, theorem 4): the quotient makes up for what the
-// rounding lost, so the result is good to a few units of the last place however small e is
+// rounding lost, so the result is good to some ten units of 2^-24 however small e is.  e = exp(-|v|) is as good for all v: what
+// the product with log2(e) loses, |v| 2^-24 of e, is put back (the rest of the product, and of log2(e), to first order).
 __device__ inline float softplus_fast(float v)
 {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(v)), u = 1.0f + e, d = u - 1.0f;
+    const float n = -fabsf(v), p = 1.44269502f * n, rest = fmaf(1.92596303e-8f, n, fmaf(1.44269502f, n, -p));
+    const float e0 = __builtin_amdgcn_exp2f(p), e = n < -128.0f ? 0.0f : fmaf(e0, 0.693147182f * rest, e0);   // (NaN stays)
+    const float u = 1.0f + e, d = u - 1.0f;
     const float l = d == 0.0f ? e : 0.69314718f * __builtin_amdgcn_logf(u) * (e * __builtin_amdgcn_rcpf(d));
     return fmaxf(v, 0.0f) + l;
 }

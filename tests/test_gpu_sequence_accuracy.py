@@ -75,3 +75,40 @@ def test_gelu_of_infinities_and_nan(S):
             S.B.linear_fwd(S.B.make_linear_desc(m, 3, 8, dtype=S.TYPES[dtype][0], act=S.B.ACT_GELU), x, w, y)
             got = S.f64(y)
             assert np.isposinf(got[:, 0]).all() and np.isnan(got[:, 1]).all() and (got[:, 2] == 0.0).all(), (dtype, m)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("step", [False, True])
+def test_softplus_holds_its_digits_for_all_sizes(S, dtype, step):
+    # One token of x = 1 and B = 1 from no state leaves delta = log(1 + exp(v)) itself, v from dt_bias.  In units of 2^-24: the
+    # exponential 3, its logarithm 3, the quotient that makes up for rounding 1 + e 6, the addition 1, the state (a sum of
+    # three parts) 2: 15, and 20 are allowed.  Exponentials below 2^-125 may come out as zero.
+    import torch
+    B, (code, ty) = S.B, S.TYPES[dtype][:2]
+    v = np.concatenate([-np.geomspace(1e-7, 100.0, 3000), np.geomspace(1e-7, 100.0, 1000), [0.0]]).astype(np.float32)
+    heads = len(v)
+    row = lambda n, value: torch.full((1, n), value, device="cuda", dtype=ty)
+    x, dt, b, y = row(heads, 1.0), row(heads, 0.0), row(1, 1.0), row(heads, 0.0)
+    a, out = torch.full((heads,), -1.0, device="cuda"), torch.empty((1, heads, 1, 1), device="cuda")
+    desc = B.make_ssm_desc(1, 1, heads, 1, 1, 1, slots=1, dtype=code)
+    call = B.ssm_scan_step if step else B.ssm_scan_fwd
+    call(desc, x, dt, a, b, b, y, dt_bias=torch.from_numpy(v).cuda(), state_out=out)
+    ref = np.logaddexp(0.0, v.astype(np.float64))
+    err = np.abs(S.f64(out).reshape(-1) - ref) / (20.0 * 2.0 ** -24 * ref + 2.0 ** -125)
+    at = int(np.argmax(err))
+    assert (err <= 1.0).all(), "%d values beyond tolerance, worst %.3g times it at %r" % ((err > 1.0).sum(), err[at], v[at])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("step", [False, True])
+def test_softplus_of_infinities_and_nan(S, dtype, step):
+    import torch
+    B, (code, ty) = S.B, S.TYPES[dtype][:2]
+    v = torch.tensor([float("-inf"), float("nan"), -200.0, 200.0], device="cuda")
+    row = lambda n, value: torch.full((1, n), value, device="cuda", dtype=ty)
+    y, out = row(4, 0.0), torch.empty((1, 4, 1, 1), device="cuda")
+    call = B.ssm_scan_step if step else B.ssm_scan_fwd
+    call(B.make_ssm_desc(1, 1, 4, 1, 1, 1, slots=1, dtype=code), row(4, 1.0), row(4, 0.0), torch.full((4,), -1.0, device="cuda"),
+         row(1, 1.0), row(1, 1.0), y, dt_bias=v, state_out=out)
+    got = S.f64(out).reshape(-1)
+    assert got[0] == 0.0 and np.isnan(got[1]) and got[2] == 0.0 and got[3] == 200.0
