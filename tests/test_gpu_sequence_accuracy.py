@@ -112,3 +112,28 @@ def test_softplus_of_infinities_and_nan(S, dtype, step):
          row(1, 1.0), row(1, 1.0), y, dt_bias=v, state_out=out)
     got = S.f64(out).reshape(-1)
     assert got[0] == 0.0 and np.isnan(got[1]) and got[2] == 0.0 and got[3] == 200.0
+
+
+@pytest.mark.parametrize("dtype,y_f32", [("bf16", False), ("f16", False), ("f32", False), ("f16", True)])
+@pytest.mark.parametrize("m", [1, 70])
+def test_silu_holds_its_digits(S, dtype, y_f32, m):
+    # v / (1 + exp(-v)): the exponent's error is (2 |v| + 1) 2^-24 of the exponential below zero in 16 bits (two roundings of
+    # v log2(e) and of log2(e) itself), the rest 8 2^-24.  In 32 bits the exponential is good to four units whatever |v| is.
+    # Below -88 results may be zero: 88 exp(-88) is 2^-120.
+    import torch
+    if dtype == "f32":
+        v = torch.from_numpy(np.concatenate([-np.geomspace(1e-6, 100.0, 5001), np.geomspace(1e-6, 100.0, 3001)]).astype(np.float32))
+    else:
+        v = torch.arange(-32768, 32768, dtype=torch.int32).to(torch.int16).view(S.TYPES[dtype][1])
+        size = v.float().abs()
+        v = v[torch.isfinite(v.float()) & (size < 100.0) & ((size > 2.0 ** -100) | (v == 0))]
+    x = S.f64(v)
+    ref = x / (1.0 + np.exp(-x))
+    got = of_every_value(S, v, dtype, "silu", y_f32, m)
+    out = "f32" if y_f32 else dtype
+    rel = ((0.0 if out == "f32" else 2.0 * np.abs(x)) + 8.0) * 2.0 ** -24
+    tol = half_spacing(ref * (1.0 + rel), out) + rel * np.abs(ref) + 2.0 ** -119
+    worst = np.abs(got - ref) / tol
+    at = np.unravel_index(np.argmax(worst), worst.shape)
+    assert (worst <= 1.0).all(), "%d values beyond tolerance, worst %.3g times it at %r" % (
+        (worst > 1.0).any(0).sum(), worst[at], float(x[at[1]]))
