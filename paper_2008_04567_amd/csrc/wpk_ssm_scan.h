@@ -139,9 +139,9 @@ __device__ inline int nth_longest(const Requests &q, int sequences, int n, int *
 }
 
 // a request has as many parts as it has chunks for, one at least
-template <typename T> __device__ inline int parts_of_request(const SsmArgs<T> &a, int chunks)
+__device__ inline int parts_of_request(int part_chunks, int n_parts, int chunks)
 {
-    return min(max((chunks + a.part_chunks - 1) / a.part_chunks, 1), a.n_parts);
+    return min(max((chunks + part_chunks - 1) / part_chunks, 1), n_parts);
 }
 
 // One part of a request: FULL computes y and the state at its end, otherwise only what its tokens add to a state.
@@ -169,66 +169,191 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
         return p + (s & 4);
     }
 
+    // The kernel's arguments where the launch left them, read again from there: what only a part's end wants would otherwise be
+    // kept in registers that its chunks have a use for.
+    typedef const __attribute__((address_space(4))) SsmArgs<T> *Again;
+    static __device__ Again arguments_again()
+    {
+        uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(at));
+        return (Again)at;
+    }
+
+    // where this workgroup's part is
+    struct Part {
+        int head, part, parts, first, length, c0, c1, slot, p;      // p: the lane's row of the head's state
+        bool resume;
+        size_t pool_at, ws_head;
+        float *ws;
+    };
+    template <typename A> static __device__ Part locate(A a, int r)
+    {
+        const Requests rq = {a->rq.starts, a->rq.slot_map, a->rq.resume, a->rq.tokens, a->rq.max_length, a->rq.slots};
+        Part w;
+        w.head = blockIdx.x % a->heads;
+        w.part = blockIdx.y;
+        request_rows(rq, r, &w.first, &w.length);
+        const int chunks = (w.length + Q - 1) / Q;
+        w.parts = parts_of_request(a->part_chunks, a->n_parts, chunks);
+        w.c0 = w.part * a->part_chunks;
+        w.c1 = w.part == w.parts - 1 ? chunks : w.c0 + a->part_chunks;
+        w.p = blockIdx.x / a->heads * 64 + (threadIdx.x >> 6) * 16 + (threadIdx.x & 15);
+        w.slot = request_slot(rq, r);
+        w.resume = a->state_in && w.slot >= 0 && request_resumes(rq, r);
+        const size_t size = (size_t)a->head_dim * a->state_dim;
+        w.pool_at = ((size_t)max(w.slot, 0) * a->heads + w.head) * size;
+        w.ws_head = (size_t)r * a->heads + w.head;
+        w.ws = a->parts ? a->parts + w.ws_head * a->n_parts * size : nullptr;
+        return w;
+    }
+
+    // the state: rows n 16 i + 4 g .. + 3 of column p (its row of the head's 64)
+    template <typename A> static __device__ void get_state(A a, int p, f32x4 (&h)[NB], const float *src, bool there)
+    {
+        const int P = a->head_dim, N = a->state_dim, g = threadIdx.x >> 4 & 3;
+        const Rows rows = rows_at(src, there ? 1 : 0, (uint32_t)(P * N) * 4);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int n = 16 * i + 4 * g, left = p < P ? N - n : 0;
+            const uint32_t at = (uint32_t)(p * N + n) * 4;
+            Piece<float, 4> v;
+            if (a->vec_state) v.template load<true>(rows, left > 0 ? at : kOutside, 4);
+            else v.template load<false>(rows, at, left);
+            h[i] = v.v;
+        }
+    }
+    template <typename A> static __device__ void put_state(A a, int p, const f32x4 (&h)[NB], float *dst, bool there)
+    {
+        const int P = a->head_dim, N = a->state_dim, g = threadIdx.x >> 4 & 3;
+        const Rows rows = rows_at(dst, there ? 1 : 0, (uint32_t)(P * N) * 4);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int n = 16 * i + 4 * g, left = p < P ? N - n : 0;
+            const uint32_t at = (uint32_t)(p * N + n) * 4;
+            Piece<float, 4> v;
+            v.v = h[i];
+            if (a->vec_state) v.template store<true>(rows, left > 0 ? at : kOutside, 4);
+            else v.template store<false>(rows, at, left);
+        }
+    }
+
+    // The state before the part.  Parts meet through the workspace: entry i holds the state behind part i (what its tokens
+    // leave, until ssm_join_kernel has added what the parts before it left), the last entry the state before the request itself,
+    // since whoever does the last part may be writing the pool's entry already.
+    template <typename A> static __device__ void get_before(A a, const Part &w, f32x4 (&h)[NB])
+    {
+        const size_t size = (size_t)a->head_dim * a->state_dim;
+        if (w.part > 0) get_state(a, w.p, h, w.ws + (size_t)(w.part - 1) * size, FULL);
+        else get_state(a, w.p, h, FULL && w.parts > 1 ? w.ws + (size_t)(a->n_parts - 1) * size : a->state_in + w.pool_at, w.resume);
+    }
+
+    // rows of W columns, `cols` of them there, as they are
+    template <int W> static __device__ void stage_plain(T *to, const T *from, int64_t stride, int cols, int left)
+    {
+        const Rows rows = rows_at(from, left, (uint32_t)stride * sizeof(T));
+        for (int task = threadIdx.x; task < Q * W / 8; task += 256) {
+            const int row = task / (W / 8), n = task % (W / 8) * 8;
+            Piece<T, 8> v;
+            v.template load<WIDE>(rows, n < cols ? (row * (uint32_t)stride + n) * sizeof(T) : kOutside, cols - n);
+            __builtin_memcpy(__builtin_assume_aligned(&to[row * W + n], 16), &v.v, sizeof(v.v));
+        }
+    }
+
+    // The part again as the definition has it, token by token in 32 bits: for values that the products cannot carry.  A wave
+    // has its 16 rows of the state as before (`mine`: unless nothing happened to them), rows of B, C and X stand in LDS as they
+    // come, and of four tokens at a time lane group g gates and stores the g-th.  One request of 16384 tokens of 32 heads of 64 x
+    // 128 numbers, bf16, with an infinity among its first: 1380 us.
+    static __device__ void walk(Again a, const Part &w, Shared &sm, bool mine, f32x4 (&h)[NB])
+    {
+        const int P = a->head_dim, N = a->state_dim, head = w.head, group = head / (a->heads / a->groups);
+        const int p_base = blockIdx.x / a->heads * 64, tid = threadIdx.x;
+        int g = tid >> 4 & 3;
+        const uint32_t e = sizeof(T), zs = (uint32_t)a->z_stride * e, ys = (uint32_t)a->y_stride * e;
+        const float rate = a->a[head], skip = a->d_skip ? a->d_skip[head] : 0.0f, dt_bias = a->dt_bias ? a->dt_bias[head] : 0.0f;
+        const int64_t hp = (int64_t)head * P;
+        typedef T tvec __attribute__((ext_vector_type(4)));
+        T *const lb = (T *)&sm.b[0][0], *const lc = (T *)&sm.c[0][0], *const lx = (T *)&sm.x[0][0];
+        static_assert(sizeof(sm.b) >= Q * NPAD * sizeof(T) && sizeof(sm.x) >= Q * 64 * sizeof(T), "room for plain rows");
+        static_assert(!FULL || sizeof(sm.c) >= Q * NPAD * sizeof(T), "room for plain rows");
+#pragma unroll 1
+        for (int chunk = w.c0; chunk < w.c1; ++chunk) {
+            const int left = min(w.length - chunk * Q, Q);
+            const int64_t t0 = w.first + chunk * Q;
+            stage_plain<NPAD>(lb, a->b + t0 * a->b_stride + group * N, a->b_stride, N, left);
+            if (FULL) stage_plain<NPAD>(lc, a->c + t0 * a->c_stride + group * N, a->c_stride, N, left);
+            stage_plain<64>(lx, a->x + t0 * a->x_stride + hp + p_base, a->x_stride, P - p_base, left);
+            if (tid < Q) {                           // (tokens that are not there change nothing)
+                float delta = 0.0f;
+                if (tid < left) {
+                    delta = (float)a->dt[(t0 + tid) * a->dt_stride + head] + dt_bias;
+                    if (a->softplus) delta = softplus(delta);
+                }
+                sm.delta[tid] = delta;
+                sm.into[tid] = tid < left ? expf(delta * rate) : 1.0f;       // (what a token keeps, here)
+            }
+            __syncthreads();
+            const Rows zrows = rows_at(a->z + t0 * a->z_stride + hp, FULL && a->z ? left : 0, zs);
+            const Rows yrows = rows_at(a->y + t0 * a->y_stride + hp, left, ys);
+            const uint32_t at_p = w.p < P ? w.p * e : kOutside;
+            Piece<T, 1> z, next, y;
+            next.template load<false>(zrows, at_p + g * zs, FULL);
+#pragma unroll 1
+            for (int t4 = 0; mine && t4 < left; t4 += 4) {
+                z = next;
+                if (FULL) next.template load<false>(zrows, at_p + (t4 + 4 + g) * zs, 1);
+                float sums[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    asm volatile("" : "+v"(g));      // (which numbers there are is found anew for every token, not held for all)
+                    const int t = t4 + u;
+                    const float keep = sm.into[t], in_x = sm.delta[t] * (float)lx[t * 64 + w.p - p_base];
+                    float s = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < NB; ++k) {
+                        const int n = 16 * k + 4 * g;
+                        const tvec b = *(const tvec *)&lb[t * NPAD + n];
+                        h[k] = h[k] * keep + __builtin_convertvector(b, f32x4) * in_x;
+                        if constexpr (FULL) {
+                            const f32x4 c = __builtin_convertvector(*(const tvec *)&lc[t * NPAD + n], f32x4);
+                            f32x4 v = h[k] * c;
+#pragma unroll
+                            for (int j = 1; j < 4 && !WIDE; ++j) v[j] = n + j < N ? v[j] : 0.0f;
+                            s += n < N ? (v[0] + v[1]) + (v[2] + v[3]) : 0.0f;       // (elsewhere infinities would meet zeros)
+                        }
+                        if (NB * sizeof(T) > 16 && k % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                    }
+                    sums[u] = s;
+                }
+                if constexpr (FULL) {
+                    // lane group g gets the whole of the g-th sum
+                    const bool g0 = g & 1, g1 = g & 2;
+                    float s01 = g0 ? sums[1] : sums[0], s23 = g0 ? sums[3] : sums[2];
+                    s01 += __shfl_xor(g0 ? sums[0] : sums[1], 16);
+                    s23 += __shfl_xor(g0 ? sums[2] : sums[3], 16);
+                    float s = g1 ? s23 : s01;
+                    s += __shfl_xor(g1 ? s01 : s23, 32);
+                    if (a->d_skip) s += skip * (float)lx[(t4 + g) * 64 + w.p - p_base];
+                    if (a->z) s *= silu_as<T>((float)z.v[0]);
+                    y.v[0] = (T)s;
+                    y.template store<false>(yrows, at_p + (t4 + g) * ys, 1);
+                }
+            }
+            __syncthreads();
+        }
+    }
+
     static __device__ void run(const SsmArgs<T> &a, Shared &sm)
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         int lane_col = lane & 15, lane_g = lane >> 4;
-        const int head = blockIdx.x % a.heads, pblock = blockIdx.x / a.heads, part = blockIdx.y;
         const int r = a.sequences ? nth_longest(a.rq, a.sequences, blockIdx.z, (int *)&sm.b[0][0]) : blockIdx.z;
-        const int P = a.head_dim, N = a.state_dim, group = head / (a.heads / a.groups);
-        int first, length;
-        request_rows(a.rq, r, &first, &length);
-        const int chunks = (length + Q - 1) / Q;
-        // this part's chunks
-        const int parts = parts_of_request(a, chunks);
-        if (FULL ? part >= parts : part >= parts - 1) return;
-        const int c0 = part * a.part_chunks, c1 = part == parts - 1 ? chunks : c0 + a.part_chunks;
-
-        const int p_base = pblock * 64;
-        const int slot = request_slot(a.rq, r);
-        const bool resume = a.state_in && slot >= 0 && request_resumes(a.rq, r);
-        const size_t state_size = (size_t)P * N, pool_at = ((size_t)max(slot, 0) * a.heads + head) * state_size;
-        const size_t ws_head = (size_t)r * a.heads + head;
-        float *const ws = a.parts ? a.parts + ws_head * a.n_parts * state_size : nullptr;
-
-        // the state: rows n 16 i + 4 g .. + 3 of column p (its row of the head's 64)
+        const Part w = locate(&a, r);
+        if (FULL ? w.part >= w.parts : w.part >= w.parts - 1) return;
+        const int head = w.head, first = w.first, length = w.length, c0 = w.c0, c1 = w.c1;
+        const int P = a.head_dim, N = a.state_dim, group = head / (a.heads / a.groups), p_base = blockIdx.x / a.heads * 64;
         f32x4 h[NB];
-        auto get_state = [&](const float *src, bool there) {
-            const Rows rows = rows_at(src, there ? 1 : 0, (uint32_t)state_size * 4);
-            const int p = p_base + wave * 16 + lane_col;
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                const int n = 16 * i + 4 * lane_g, left = p < P ? N - n : 0;
-                const uint32_t at = (uint32_t)(p * N + n) * 4;
-                Piece<float, 4> v;
-                if (a.vec_state) v.template load<true>(rows, left > 0 ? at : kOutside, 4);
-                else v.template load<false>(rows, at, left);
-                h[i] = v.v;
-            }
-        };
-        auto put_state = [&](float *dst, bool there) {
-            const Rows rows = rows_at(dst, there ? 1 : 0, (uint32_t)state_size * 4);
-            const int p = p_base + wave * 16 + lane_col;
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                const int n = 16 * i + 4 * lane_g, left = p < P ? N - n : 0;
-                const uint32_t at = (uint32_t)(p * N + n) * 4;
-                Piece<float, 4> v;
-                v.v = h[i];
-                if (a.vec_state) v.template store<true>(rows, left > 0 ? at : kOutside, 4);
-                else v.template store<false>(rows, at, left);
-            }
-        };
-        // The state before the part.  Parts meet through the workspace: entry i holds the state behind part i (what its
-        // tokens leave, until ssm_join_kernel has added what the parts before it left), the last entry the state before the
-        // request itself, since whoever does the last part may be writing the pool's entry already.
-        if (part == 0) {
-            float *const before = ws + (size_t)(a.n_parts - 1) * state_size;
-            get_state(FULL && parts > 1 ? before : a.state_in + pool_at, resume);
-            if (!FULL) put_state(before, resume);
-        } else {
-            get_state(ws + (size_t)(part - 1) * state_size, FULL);
-        }
+        get_before(&a, w, h);
+        if (!FULL && w.part == 0) put_state(&a, w.p, h, w.ws + (size_t)(a.n_parts - 1) * P * N, w.resume);
 
         const float rate = a.a[head], skip = a.d_skip ? a.d_skip[head] : 0.0f, dt_bias = a.dt_bias ? a.dt_bias[head] : 0.0f;
         const int64_t hp = (int64_t)head * P;
@@ -330,7 +455,7 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
             if constexpr (FULL) fetch_rows(rc, cp, a.c_stride, cs, c0);
             fetch_x(c0);
         }
-        const bf16x8 zero8 = {0, 0, 0, 0, 0, 0, 0, 0};
+        float odd = 0.0f;                                // NaN once there was an infinity or NaN in y before its gate
         for (int chunk = c0; chunk < c1; ++chunk) {
             stage();
             if (wave == 0) scalars(chunk);
@@ -443,12 +568,6 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
                     const bf16x4 hi = read_transposed(&sm.x[q][(32 * k + 4) * 64 + (at_x ^ 8)]);
                     fx[k][q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                 }
-            // Infinities or NaN among x may not meet the zeros of M that stand for later tokens: x times zero finds them.
-            f32x4 odd = {0, 0, 0, 0};
-            if constexpr (FULL)
-#pragma unroll
-                for (int k = 0; k < QK; ++k) odd = mma(fx[k][0], zero8, odd);
-
             // the state behind the chunk
 #pragma unroll
             for (int i = 0; i < NB; ++i) h[i] *= keep;
@@ -482,38 +601,17 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
             }
 
             if constexpr (FULL) {
-                if (!__any(odd[0] != 0.0f || odd[1] != 0.0f || odd[2] != 0.0f || odd[3] != 0.0f)) {
 #pragma unroll
-                    for (int k = 0; k < QK; ++k) {
-                        bf16x8 fm[QB][YP];
+                for (int k = 0; k < QK; ++k) {
+                    bf16x8 fm[QB][YP];
 #pragma unroll
-                        for (int i = 2 * k; i < QB; ++i)
+                    for (int i = 2 * k; i < QB; ++i)
 #pragma unroll
-                            for (int q = 0; q < YP; ++q) fm[i][q] = *(const bf16x8 *)&sm.m[q][m_at(16 * i + col, 32 * k + 8 * g)];
-                        each_pair<YP, NP, YP>([&](int u, int v) {
+                        for (int q = 0; q < YP; ++q) fm[i][q] = *(const bf16x8 *)&sm.m[q][m_at(16 * i + col, 32 * k + 8 * g)];
+                    each_pair<YP, NP, YP>([&](int u, int v) {
 #pragma unroll
-                            for (int i = 2 * k; i < QB; ++i) acc[i] = mma(fx[k][u], fm[i][v], acc[i]);
-                        });
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < QB; ++i) {
-                        const int t = 16 * i + col;
-#pragma unroll 1
-                        for (int s = 0; s <= t; ++s) {
-                            float m = 0.0f;
-#pragma unroll
-                            for (int q = 0; q < YP; ++q) m += (float)sm.m[q][m_at(t, s & ~3) + (s & 3)];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const int p = wave * 16 + 4 * g + j;
-                                float x = 0.0f;
-#pragma unroll
-                                for (int q = 0; q < NP; ++q) x += (float)sm.x[q][piece_at<8>(s, p >> 3) + (p & 7)];
-                                acc[i][j] = fmaf(m, x, acc[i][j]);
-                            }
-                        }
-                    }
+                        for (int i = 2 * k; i < QB; ++i) acc[i] = mma(fx[k][u], fm[i][v], acc[i]);
+                    });
                 }
                 const Rows yrows = rows_at(a.y + (int64_t)(first + t0) * a.y_stride + hp, left, ys);
 #pragma unroll
@@ -522,6 +620,7 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float v = acc[i][j];
+                        odd = fmaf(v, 0.0f, odd);
                         if (a.z) v *= silu_as<T>((float)rz[i].v[j]);
                         out.v[j] = (T)v;
                     }
@@ -530,12 +629,27 @@ template <typename T, int NPAD, int Q, bool FULL, bool WIDE> struct SsmScan {
             }
             __syncthreads();
         }
-        asm volatile("" : "+v"(lane_col), "+v"(lane_g));
+        // An infinity or NaN among the operands, numbers beyond the largest bf16 one, sums that overflow: parts of an infinity do
+        // not add up to it, and x of a token meets the zeros of M for the tokens before.  Any of it shows in y or in the state.
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) odd = fmaf(h[i][j], 0.0f, odd);
+        const bool mine = __any(odd != 0.0f);
+        if (lane == 0) sm.block[wave] = mine ? 1.0f : 0.0f;
+        __syncthreads();
+        const f32x4 any = *(const f32x4 *)&sm.block[0];
+        if (__builtin_amdgcn_readfirstlane(any[0] + any[1] + any[2] + any[3] != 0.0f)) {
+            const Again again = arguments_again();
+            const Part v = locate(again, r);
+            if (mine) get_before(again, v, h);
+            walk(again, v, sm, mine, h);
+        }
         if (!FULL) {
-            put_state(ws + (size_t)part * state_size, true);
-            if (pblock == 0 && tid == 0) a.part_decay[ws_head * a.n_parts + part] = total;
-        } else if (part == parts - 1) {
-            put_state(a.state_out + pool_at, a.state_out && slot >= 0);
+            put_state(&a, w.p, h, w.ws + (size_t)w.part * P * N, true);
+            if (p_base == 0 && tid == 0) a.part_decay[w.ws_head * a.n_parts + w.part] = total;
+        } else if (w.part == w.parts - 1) {
+            put_state(&a, w.p, h, a.state_out + w.pool_at, a.state_out && w.slot >= 0);
         }
     }
 };
@@ -552,6 +666,9 @@ ssm_scan_kernel(SsmArgs<T> a)
     Scan::run(a, sm);
 }
 
+// What a part keeps of a number: an infinity stays one, also where the part's tokens together keep nothing in 32 bits.
+__device__ inline float kept(float v, float decay) { return decay == 0.0f && fabsf(v) > 3.4028234e38f ? v : v * decay; }
+
 // From what the parts' tokens leave to the states behind the parts: entry i of the workspace += decay of part i times entry
 // i - 1, a lane to four numbers of a state.
 template <typename T, int Q> __global__ void __launch_bounds__(256) ssm_join_kernel(SsmArgs<T> a)
@@ -559,7 +676,7 @@ template <typename T, int Q> __global__ void __launch_bounds__(256) ssm_join_ker
     const int head = blockIdx.y, r = blockIdx.z;
     int first, length;
     request_rows(a.rq, r, &first, &length);
-    const int parts = parts_of_request(a, (length + Q - 1) / Q);
+    const int parts = parts_of_request(a.part_chunks, a.n_parts, (length + Q - 1) / Q);
     const int64_t size = (int64_t)a.head_dim * a.state_dim, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (parts < 3 || at >= size) return;
     const int64_t ws_head = (int64_t)r * a.heads + head;
@@ -574,14 +691,15 @@ template <typename T, int Q> __global__ void __launch_bounds__(256) ssm_join_ker
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (i + j >= parts - 1) break;
-                cur = cur * decay[i + j] + e[j];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) cur[k] = kept(cur[k], decay[i + j]) + e[j][k];
                 *(f32x4 *)(ws + (i + j) * size) = cur;
             }
         }
     } else {
         for (int c = 0; c < 4 && at + c < size; ++c) {
             float cur = ws[c];
-            for (int i = 1; i < parts - 1; ++i) ws[i * size + c] = cur = cur * decay[i] + ws[i * size + c];
+            for (int i = 1; i < parts - 1; ++i) ws[i * size + c] = cur = kept(cur, decay[i]) + ws[i * size + c];
         }
     }
 }
