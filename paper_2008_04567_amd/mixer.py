@@ -4,7 +4,11 @@
 
 ``Mixer`` owns the weights and a pool of states (one entry per request: the convolution's last inputs and the scan's
 state); ``prompt`` takes the ragged prompts of some requests, ``step`` one token of each.  Tensors and streams are
-PyTorch's; every operation is the library's.
+PyTorch's; every operation is the library's.  An example: its weights are random, and it is the four calls alone, without
+the normalisations that models put around and into such a layer.
+
+What a call returns is the plan's own buffer: it holds until the plan's next call.  A plan's calls share buffers and
+workspace, so they belong on one stream, or in order; so do calls of any plans that use the same entries of the pool.
 
 ``python -m paper_2008_04567_amd.mixer`` takes a batch of prompts through a layer, continues them token by token with the
 step captured in a HIP graph, and prints what both take.
@@ -46,20 +50,46 @@ class Mixer:
         return _Plan(self, sequences, tokens, max_length)
 
     def prompt(self, plan, h, starts, slot_map, resume=None, stream=None):
-        """Rows of the requests' tokens one after another; resume: which continue from their states (int32, all start
-        afresh without)."""
+        """h: rows of the requests' tokens one after another, [tokens][width] (rows may be slices of longer ones).  starts
+        [requests + 1], slot_map [requests] and resume [requests] are int32 on the GPU: without starts every request has the
+        plan's max_length tokens, without slot_map request i has entry i, without resume all start afresh."""
         if resume is None:
             resume = plan.fresh
+        h = self._check(plan, h, slot_map, starts=(starts, plan.sequences + 1), resume=(resume, plan.sequences))
         return plan.run(h, starts, slot_map, resume, False, stream)
 
     def step(self, plan, h, slot_map, stream=None):
         """One token of every request, row i that of request i."""
+        if plan.tokens != plan.sequences or plan.max_length != 1:
+            raise ValueError("the plan is not one of a token a request")
+        h = self._check(plan, h, slot_map)
         return plan.run(h, None, slot_map, None, True, stream)
+
+    def _check(self, plan, h, slot_map, **others):
+        """What the library cannot see from addresses.  Returns the rows of h."""
+        if plan.m is not self:
+            raise ValueError("the plan is another layer's")
+        want = (plan.tokens, self.width)
+        if h.dim() != 2 and h.is_contiguous() and h.shape[-1] == self.width:
+            h = h.view(-1, self.width)
+        if tuple(h.shape) != want or h.dtype != self.dtype or h.device != self.w_in.device:
+            raise ValueError("h is %s %s on %s, not %s %s on %s" % (tuple(h.shape), h.dtype, h.device, want, self.dtype,
+                                                                    self.w_in.device))
+        if h.stride(1) != 1 or (plan.tokens > 1 and h.stride(0) < self.width):
+            raise ValueError("h: values of a row stand one after another, rows apart")
+        for name, (t, n) in dict(others, slot_map=(slot_map, plan.sequences)).items():
+            if t is not None and not (torch.is_tensor(t) and t.dtype == torch.int32 and tuple(t.shape) == (n,) and t.is_contiguous() and
+                    t.device == h.device):
+                raise ValueError("%s is not %d int32 numbers on %s" % (name, n, h.device))
+        if not h.is_cuda:
+            raise ValueError("the layer is not on the GPU")
+        return h
 
 
 class _Plan:
     def __init__(self, m, sequences, tokens, max_length):
         self.m, inner, gn = m, m.inner, m.groups * m.state_dim
+        self.sequences, self.tokens, self.max_length = sequences, tokens, max_length
         empty = lambda *shape, dtype=m.dtype: torch.empty(shape, device=m.device, dtype=dtype)
         self.row, self.conv, self.y, self.out = (empty(tokens, m.row), empty(tokens, m.conv_channels), empty(tokens, inner),
                                                  empty(tokens, m.width))
@@ -80,6 +110,7 @@ class _Plan:
     def run(self, h, starts, slot_map, resume, step, stream):
         m = self.m
         s = stream if stream is not None else torch.cuda.current_stream()
+        self.lin_in.x_stride = self.lin_out.residual_stride = h.stride(0) if self.tokens > 1 else m.width
         B.linear_fwd(self.lin_in, h, m.w_in, self.row, workspace=self.workspace, stream=s)
         conv = dict(bias=m.b_conv, slot_map=slot_map, state_in=m.conv_state, state_out=m.conv_state, stream=s)
         scan = dict(d=m.d, z=self.z, dt_bias=m.dt_bias, slot_map=slot_map, state_in=m.scan_state, state_out=m.scan_state,
