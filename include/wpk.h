@@ -440,13 +440,16 @@ const char *wpk_version(void);
  * Tensors are DEVICE pointers owned by the caller, of the descriptor's dtype unless a type is given, aligned to
  * their element.  Rows are one per token, dense within, `*_stride` elements apart, so a tensor may be a slice of
  * longer rows (16-byte aligned rows are read faster).  Outputs may not overlap inputs except where stated.
- * All sums and states are held in 32 bits; values are rounded once, when stored.
+ * All sums and states are held in 32 bits; values are rounded once, when stored.  One exception: on the way to a y of 16 bits,
+ * prompts of the scan take the operands of two products, decayed C B^T and the state that C reads, with 17 bits (2^-17 of
+ * each; y's own rounding is 2^-9 or 2^-12).  What goes into the state keeps all bits, and so does everything for fp32.
+ * Infinities and NaN leave what the definitions below say, where these are computed in 32 bits.
  *
  * Requests ("sequences").  The tokens of all requests stand one after another.  `starts` is NULL (every request has
  * max_length tokens) or sequences + 1 ascending int32 ON THE DEVICE: request i has the rows starts[i] .. starts[i+1]-1,
  * possibly none.  Values outside 0 .. tokens are clamped to it.  max_length shapes the launch; a request longer than
- * it is still computed in full.  Rows of no request are left alone.  `tokens` (and a product's rows and columns) may
- * be 2^30 at most.
+ * it is still computed in full.  Rows of no request are left alone.  `tokens` (and a product's rows) may be 2^30
+ * at most.
  *
  * States.  A pool has `slots` entries; request i has entry slot_map[i] (int32 on the device; NULL: entry i).  An entry
  * outside 0 .. slots-1 means that the request starts from zero and leaves no state.  Entries of different requests have
@@ -465,7 +468,7 @@ typedef struct wpk_linear_desc {
     int32_t y_dtype;                /* dtype or WPK_F32                                                 */
     int32_t act;                    /* WPK_ACT_*                                                        */
     int64_t x_stride, w_stride;     /* elements between rows, >= k, below 2^20                          */
-    int64_t y_stride, residual_stride;   /* >= n                                                        */
+    int64_t y_stride, residual_stride;   /* >= n, below 2^20, also without a residual                   */
 } wpk_linear_desc;
 
 /* Bytes of workspace that wpk_linear_fwd needs for this descriptor (0: none), or a negative status.  Host only. */
@@ -485,7 +488,7 @@ typedef struct wpk_causal_conv_desc {
     int32_t slots;                  /* entries of the state pool (0 without one)                        */
     int32_t dtype;
     int32_t act;                    /* WPK_ACT_NONE or WPK_ACT_SILU                                     */
-    int64_t x_stride, y_stride;     /* elements between rows, >= channels                               */
+    int64_t x_stride, y_stride;     /* elements between rows, >= channels (below 2^30), below 2^40      */
 } wpk_causal_conv_desc;
 
 /* w [channels][width], bias [channels] or NULL */
