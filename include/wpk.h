@@ -449,7 +449,7 @@ const char *wpk_version(void);
  * max_length tokens) or sequences + 1 ascending int32 ON THE DEVICE: request i has the rows starts[i] .. starts[i+1]-1,
  * possibly none.  Values outside 0 .. tokens are clamped to it.  max_length shapes the launch; a request longer than
  * it is still computed in full.  Rows of no request are left alone.  `tokens` (and a product's rows) may be 2^30
- * at most.
+ * at most, requests and heads 65535.
  *
  * States.  A pool has `slots` entries; request i has entry slot_map[i] (int32 on the device; NULL: entry i).  An entry
  * outside 0 .. slots-1 means that the request starts from zero and leaves no state.  Entries of different requests have

@@ -26,3 +26,14 @@ def test_conv_strides(name):
 def test_ssm_strides(name):
     assert status(B.ssm_workspace, B.make_ssm_desc(**SSM, **{name: (1 << 22) - 1})) == B.OK
     assert status(B.ssm_workspace, B.make_ssm_desc(**SSM, **{name: 1 << 22})) == B.E_UNSUPPORTED
+
+
+def test_requests_and_heads():
+    most = 65535
+    for n, code in ((most, B.E_NULL_PTR), (most + 1, B.E_UNSUPPORTED)):
+        desc = B.make_causal_conv_desc(**dict(CONV, sequences=n, tokens=n, max_length=1))
+        assert status(B.causal_conv1d_fwd, desc, None, FAKE, FAKE) == code
+        desc = B.make_ssm_desc(**dict(SSM, sequences=n, tokens=n, max_length=1))
+        assert status(B.ssm_scan_step, desc, None, *[FAKE] * 5) == code
+        desc = B.make_ssm_desc(**dict(SSM, heads=n, groups=1, head_dim=1))
+        assert status(B.ssm_scan_fwd, desc, None, *[FAKE] * 5, starts=FAKE, workspace=FAKE) == code
