@@ -3,8 +3,8 @@
 // y[t][c] = act(bias[c] + sum_j w[c][j] x[t - (W-1) + j][c]).  Bound by memory: every value is read once and written
 // once for W multiply-adds.  A lane owns V channels (16 bytes where rows start at multiples of four) and a run of kRun tokens: it
 // keeps the last W - 1 rows in registers, so rows are read W - 1 times more than once per run only, and asks for kAhead
-// rows at once.  16384 ragged tokens of 4352 bf16 channels: 62 us, 4.6 TB/s (before its weights were read by vectors, 66; so
-// measured, runs of 16 took 67, four rows at once 72, two 80).
+// rows at once.  16384 ragged tokens of 4352 bf16 channels: 62 us, 4.6 TB/s, the kernel alone, and 68 (4.2 TB/s) a call behind
+// others (before its weights were read by vectors, 66 alone; so measured, runs of 16 took 67, four rows at once 72, two 80).
 #include "wpk_seq.h"
 
 namespace wpk {

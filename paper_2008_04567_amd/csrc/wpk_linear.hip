@@ -291,9 +291,10 @@ __device__ inline void put_tile(const LinearArgs &a, const f32x16 (&acc)[TM][TN]
 // BM rows of y (columns of the MFMA) by BN columns, WM x WN waves of 32 x 32 blocks.  A step's operands are held in registers
 // while the step before is multiplied, and go to LDS (fp32's cut into their parts on the way) between two meetings of the
 // waves.  One LDS buffer: workgroups that share a compute unit fill each other's pauses, which for fp32, whose cutting takes
-// two thirds of the products' time, was worth more than a second buffer.  777 x 1000 x 2048 in fp32: 33 us and 4 for the join,
-// 86 TFLOP/s, where six bf16 products would take 12 at the rate of large ones: the cutting (six and a half vector
-// instructions an element, again by every tile that reads it) is what it spends its time on.
+// two thirds of the products' time, was worth more than a second buffer.  777 x 1000 x 2048 in fp32: 36.3 us with its join (a
+// kernel of 4 to 5 us), 88 TFLOP/s, where six bf16 products would take 12 at the rate of large ones: the cutting (six and a half
+// vector instructions an element, again by every tile that reads it) has the vector units busy for 36 % of the time, the
+// products the matrix pipes for 21 %, and neither fills the other's pauses.
 template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN) linear_tiles_kernel(LinearArgs a)
 {
     typedef typename TileType<T>::part_t part_t;
@@ -409,10 +410,11 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
 // The same for 16-bit operands in aligned rows: loads write LDS directly and take no registers, STAGES - 1 steps of BK entries
 // ahead of the products.  A wave's load brings 1024 bytes of whole rows.  The 16-byte pieces of a row stand in the order of their
 // number xor some bits of the row's, which the lanes bring about by what they ask for: 16 lanes that read the same piece of
-// neighbouring rows take all banks.  16384 x 4096 x 4096, bf16: 475 us, 1.16 PFLOP/s, the matrix pipes busy 58 % of the time
-// (a large library product reaches 1.3 to 1.5 there); 1777 x 2304 x 1544, f16, GELU: 22.5 us, of which 0.65 a
-// step of 64: its 32 KiB a compute unit come at 12.7 TB/s in all from the caches.  (Waves of 64 x 64, two to a block, that read a
-// third less of LDS took as long.)
+// neighbouring rows take all banks.  16384 x 4096 x 4096, bf16: 471 us, 1.17 PFLOP/s, the matrix pipes busy 61 % of the time
+// (a library product takes 354 to 420); 1777 x 2304 x 1544, f16, GELU: 23.5 us, of which 0.65 a step of 64.  What bounds a step is
+// not known: matrix pipes 22 %, vector units 23 % busy, waves waiting for 27 % of their time; the 32 KiB of a step come at 12.5
+// bytes a clock a compute unit, 87 % from the L2 caches, 340 clocks a request.  (Waves of 64 x 64, two to a block, that read a third
+// less of LDS took as long.)
 template <typename T, int BM, int BN, int WM, int WN, int BK, int STAGES>
 __global__ void __launch_bounds__(64 * WM * WN, (BM + BN) * BK * STAGES * 2 > 81920 ? WM * WN / 4 : WM * WN / 2)
 linear_direct_kernel(LinearArgs a)
@@ -517,7 +519,14 @@ linear_direct_kernel(LinearArgs a)
 }
 
 // ---- which of them ------------------------------------------------------------------------------------------------
-static const int kRowsMost = 64;      // rows of x that the row kernel takes
+// Rows of x that the row kernel takes.  32 rows by 8512 columns of 2048 take 10.8 us in bf16 and 26.5 in fp32, 65 (two rows of
+// tiles) 15.4 and 50.  Between, neither way is the faster throughout; 64 rows by the row kernel and by tiles, us:
+//   columns x reduction   1024 x 512   1024 x 2048   8512 x 512   8512 x 2048   4096 x 8192
+//   bf16                   5.0   5.2   11.3    8.7    6.5   5.4   14.8   10.9   37.4   16.9
+//   fp32                   7.8  16.8   24.2   19.9   22.7  16.8   48.2   32.8   81.2   45.6
+// so tiles would gain where reductions are long, and lose half in fp32 where they are not.  (The row kernel's fp32 form for 33
+// rows on keeps 6 to 62 registers in scratch memory.)
+static const int kRowsMost = 64;
 struct LinearShape {
     int tile;                         // rows and columns of a tile; 0: the row kernel
     int width;                        // of a workgroup of the row kernel

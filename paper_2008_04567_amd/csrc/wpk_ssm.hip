@@ -120,9 +120,10 @@ struct ScanShape {
 
 // Requests are cut along their tokens where their heads alone would leave compute units idle, or where the longest one would
 // still be walked through when the others are long done.  Every part but a request's last is walked through twice, first
-// for the state that it leaves and then for y, which costs half as much again.  32 heads of 64 x 128 numbers, bf16: one
-// request of 16384 tokens takes 1050 us whole and 170 in 16 parts; 24 uneven ones, 12000 tokens together (64 heads), 284 us
-// whole, the longest first, and 247 in up to three parts.
+// for the state that it leaves and then for y, which costs half as much again.  Heads of 64 x 128 numbers, bf16, calls whole and
+// cut in turn: one request of 16384 tokens (32 heads) 1078 and 177 us, of 2048 138 and 42, of 512 38 and 33; 24 uneven ones, 12000
+// tokens together, the longest 3833 (64 heads), 274 and 232; eight of 250 beside one of 3000 (32 heads) 209 and 68.  24 even ones
+// (64 heads) stay whole: 170.
 static ScanShape scan_shape(const wpk_ssm_desc &d)
 {
     const int64_t units = (longest_request(d.tokens, d.max_length) + kPartUnit - 1) / kPartUnit;
@@ -167,10 +168,12 @@ template <typename T, int NPAD, int Q, bool WIDE> static int launch_scan_rows(Ss
 }
 
 // Chunks of 64 tokens where two workgroups of them fit a compute unit, else of 32: 32 heads of 64 numbers, 16384 tokens,
-// bf16, states of 128: 151 us by 64 and 168 by 32; of 256: 288 and 387; f16, of 64: 155 and 173; of 128: 273 and 233.  But a
-// workgroup that has its compute unit to itself gains nothing by smaller ones: f16, 10 heads of 48 x 72, 9 requests of 1001
-// tokens together, 32 us by 64 and 40 by 32.  Rows that are moved element by element take more registers: bf16, of 128: 535
-// and 338; of 256: 1025 and 820.
+// bf16, states of 128: 155 us by 64 and 183 by 32; of 256: 313 and 344; f16, of 64: 157 and 179; of 128: 277 and 243.  But a
+// workgroup that has its compute unit to itself gains nothing by smaller ones, f16: 10 heads of 48 x 72, 9 requests of 1001
+// tokens together, 32.5 us by 64 and 36.9 by 32; states of 64 x 128, 1000 tokens of 64 heads, 50 and 55; 8192 of 4 heads, 55 and
+// 60; 8 requests of 400 of 32 heads, 49 and 51, of 64, 12.6 both.  Rows that are moved element by element take more registers:
+// bf16, of 128: 543 and 357; of 256: 1017 and 792 (its kernels for 16 bits keep some 40 registers in scratch memory, at two
+// workgroups a compute unit).
 template <typename T, int NPAD> static int launch_scan(const SsmArgs<T> &a, int sequences, hipStream_t st)
 {
     const int Q = sizeof(T) == 4 || (SsmType<T>::parts == 2 && NPAD > 64) ? 32 : 64;

@@ -14,13 +14,18 @@
 // 16-byte pieces depends on the row, so that neither whole pieces nor transposing reads meet a bank twice.  The next chunk's rows come into
 // registers while this one is worked on.
 //
-// Bound by issue and by what waits on it: a chunk of 64 tokens by 128 state numbers costs a wave some 930 vector instructions
-// (decays, splitting into parts, offsets) beside 106 MFMAs, and what one wave of a SIMD spends the others cannot.  16384 tokens
-// of 32 heads of 64 x 128 numbers, bf16: 118 us for this pass (vector units 49 % busy, matrix pipes 20 %, LDS conflicts 11 %
-// of its time, from C's reads, which the compiler joins two rows apart by 16 to one: 1.8 TB/s), 46 for the one that leaves the parts' states.  Two workgroups a compute unit with all operands under
-// way in registers: three, with rows fetched late, took 178 us in all instead of 170.  Four heads of a group in a workgroup,
-// sharing G, took as long as one by one; a wave that forms the next chunk's decays beside the others' products 175; transposed
-// copies of B and X in LDS, written on the way in, 168, and 259 instead of 247 for 24 ragged requests.
+// No unit is busy all the time: 16384 tokens of 32 heads of 64 x 128 numbers, bf16, take 119 us in this pass (kernels alone,
+// under a profiler), the vector units busy for 50 % of it, LDS for 35 % (a third of that conflicts, from C's reads, which the
+// compiler joins two rows apart by 16 to one), the matrix pipes for 19 %, and waves wait for 24 % of theirs.  A chunk of 64 tokens
+// costs a wave some 910 vector instructions (decays, splitting into parts, offsets), 113 of LDS and 102 MFMAs between its
+// barriers, and a SIMD has two waves to fill them.  The pass that leaves the parts' states takes 47 us, their join 8.
+//
+// Two workgroups a compute unit with all operands under way in registers.  Measured on the way here, all kernels of such a call
+// summed under the profiler: three workgroups, with rows fetched late, 178 us instead of 170; a wave that forms the next chunk's
+// decays beside the others' products 175; transposed copies of B and X in LDS, written on the way in, 168, but 259 instead of 247
+// for 24 ragged requests.  Four heads of a group in a workgroup, sharing G, took as long as one by one.  (A head of other than 64
+// rows shares worse: of 32, two waves of four multiply zeros, 268 us instead of 152 for twice as many heads; of 128, two
+// workgroups form the same G, 152 us for half as many.)
 //
 // Types.  Operands are taken as sums of bf16 numbers: one for bf16, two for fp16 (exact), three for fp32.  What is formed
 // in fp32 on the way keeps two of them (2^-17 of it) where y is rounded to 16 bits, and three (all 24 bits) for fp32 and
