@@ -412,8 +412,8 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
 // number xor some bits of the row's, which the lanes bring about by what they ask for: 16 lanes that read the same piece of
 // neighbouring rows take all banks.  16384 x 4096 x 4096, bf16: 471 us, 1.17 PFLOP/s, the matrix pipes busy 61 % of the time
 // (a library product takes 354 to 420); 1777 x 2304 x 1544, f16, GELU: 23.5 us, of which 0.65 a step of 64.  What bounds a step is
-// not known: matrix pipes 22 %, vector units 23 % busy, waves waiting for 27 % of their time; the 32 KiB of a step come at 12.5
-// bytes a clock a compute unit, 87 % from the L2 caches, 340 clocks a request.  (Waves of 64 x 64, two to a block, that read a third
+// not known: matrix pipes 22 %, vector units 23 % busy, waves waiting for 27 % of their time; the 32 KiB of a step come at 21
+// bytes a clock a compute unit, 87 % of the requests met by the L2 caches, 340 clocks each.  (Waves of 64 x 64, two to a block, that read a third
 // less of LDS took as long.)
 template <typename T, int BM, int BN, int WM, int WN, int BK, int STAGES>
 __global__ void __launch_bounds__(64 * WM * WN, (BM + BN) * BK * STAGES * 2 > 81920 ? WM * WN / 4 : WM * WN / 2)
