@@ -34,8 +34,8 @@
  *     share it and must run one after another (one stream, or ordered streams).
  *   - The library never falls back to the CPU: without a usable GPU every compute entry point
  *     returns WPK_E_HIP.
- *   - The sequence layers at the end of this file (wpk_linear_*, wpk_causal_conv1d_*, wpk_ssm_*) keep no
- *     scratch, take no lock and never allocate: what room a call needs is the caller's `workspace`, so calls
+ *   - The sequence layers at the end of this file (wpk_linear_*, wpk_causal_conv1d_*, wpk_ssm_*) and what stands
+ *     around them (wpk_rms_norm_*, wpk_quantize_*, wpk_linear_q8_*, wpk_grouped_linear_*, wpk_route_*) keep no scratch, take no lock and never allocate: what room a call needs is the caller's `workspace`, so calls
  *     on different streams may overlap wherever their tensors and workspaces differ, and any call may be
  *     recorded by a stream capture.  Their conventions stand with them.
  */
@@ -62,8 +62,9 @@ enum {
     WPK_E_TOO_LARGE   = -9  /* wpk_conv2d_fwd_noalloc: the layer's packed weights exceed the static scratch */
 };
 
-/* Element types.  Convolutions take WPK_F32 alone; the sequence layers take all three. */
-enum { WPK_F32 = 0, WPK_BF16 = 1, WPK_F16 = 2 };
+/* Element types.  Convolutions take WPK_F32 alone; the sequence layers take the first three; WPK_E4M3, 8 bits with four of exponent
+ * and three of mantissa (largest 448, NaN, no infinity), is what the 8-bit products at the end of this file read. */
+enum { WPK_F32 = 0, WPK_BF16 = 1, WPK_F16 = 2, WPK_E4M3 = 3 };
 /* Activation layouts.  Bit 0: x is channels-last [N][H][W][C]; bit 1: y (and a fused residual) is
  * channels-last [N][P][Q][K].  Weights are always [K][C][R][S].  The two mixed values make the
  * kernel that computes a layer also transform the layout (Section 2.1, data layout transformation)
@@ -530,6 +531,134 @@ int wpk_ssm_scan_fwd(const wpk_ssm_desc *d, const void *x, const void *dt, const
 int wpk_ssm_scan_step(const wpk_ssm_desc *d, const void *x, const void *dt, const float *a, const void *b, const void *c,
                       const float *d_skip, const void *z, const float *dt_bias, const int32_t *slot_map,
                       const float *state_in, float *state_out, void *y, void *stream);
+
+/* ---- around a mixer layer: normalisation, 8-bit products, experts ---------------------------------- */
+/*
+ * What a served model puts around and between its sequence layers: the RMS norm with the residual's addition, matrix products
+ * in 8 bits, and layers of experts (a router and products of rows sorted by expert).  The conventions are the sequence layers':
+ * device pointers owned by the caller, rows dense within and `*_stride` elements apart, sums in 32 bits, values rounded once, when
+ * stored, nothing allocated or kept, any call can be captured.  Tensors and stream belong to the current device.
+ *
+ * 8 bits.  A row of e4m3 values q has one fp32 scale for each 128 of them, rows of scales `*_scale_stride` elements apart: the row
+ * stands for q[c] * scale[c / 128].  The last block may be shorter.  A weight has one scale for each block of 128 rows and 128
+ * columns: row j stands for q[j][c] * scale[j / 128][c / 128].  Rows of 8-bit values start at multiples of 16 bytes (pointers and
+ * strides); what is behind a row's values, up to the next multiple of 16, is not used and not written.
+ * From a row v in 32 bits they are made so: scale = max |v| of the block / 448, at least 2^-110, inverse = 1 / scale, q = v * inverse
+ * rounded to the nearest e4m3 number, ties to even, none beyond 448.  A NaN stays one and leaves the rest of its block alone; a
+ * block with an infinity has an infinite scale, and no value of it means a number.
+ * Products of 8-bit values into a y of 16 bits add eight neighbouring entries' products with 13 bits below the largest of them (a
+ * sum is off by some 2e-5 of itself; y's own rounding is 2^-9 or 2^-12); into a y of 32 bits they are added in 32 bits.
+ */
+
+/* For every row t, with `parts` rows of x to it:
+ *   s[t] = residual[t] + sum_j weights[t][j] * x[source[t][j]]     j < parts; without weights all are 1, without source the row is
+ *                                                                  t * parts + j, without a residual it is zero
+ *   h[t] = s[t]                                                    the residual stream behind the addition
+ *   v[t][c] = s[t][c] / sqrt(mean of s[t]^2 over c's group + eps) * gain[c]
+ *   y[t] = v[t], and q[t], scales[t] = v[t] in 8 bits              from the unrounded s
+ * A row has `groups` equal groups, each with a mean of its own.  Values of source outside 0 .. x_rows-1 add nothing. */
+typedef struct wpk_rms_norm_desc {
+    int32_t rows, width;            /* rows (0 is allowed, 2^30 at most), columns (65536 at most)        */
+    int32_t groups;                 /* width % groups == 0; a group's width % 128 == 0 where q is given and groups > 1 */
+    int32_t parts, x_rows;          /* rows of x that make one (1 .. 64); rows that x has                */
+    int32_t dtype;                  /* of x, residual, gain, h and y: WPK_F32, WPK_BF16 or WPK_F16       */
+    float eps;                      /* >= 0                                                              */
+    int64_t x_stride, residual_stride, h_stride, y_stride, q_stride;   /* >= width, below 2^30; q's % 16 == 0 */
+    int64_t scale_stride;           /* >= blocks of 128, below 2^30                                      */
+} wpk_rms_norm_desc;
+
+/* x [x_rows][width], source int32 [rows][parts] or NULL, weights fp32 [rows][parts] or NULL, residual [rows][width] or NULL,
+ * gain [width] or NULL (all ones); h, y, q with scales: any of them NULL, not all.  h may be the residual itself, y or h x
+ * itself where parts is 1 and source NULL, y the residual or h no other (same stride for what is the same). */
+int wpk_rms_norm_fwd(const wpk_rms_norm_desc *d, const void *x, const int32_t *source, const float *weights,
+                     const void *residual, const void *gain, void *h, void *y, void *q, float *scales, void *stream);
+
+/* q, scales = x in 8 bits. */
+typedef struct wpk_quantize_desc {
+    int32_t rows, width;            /* rows (0 is allowed, 2^30 at most), columns (2^30 at most)         */
+    int32_t dtype;                  /* of x: WPK_F32, WPK_BF16 or WPK_F16                                */
+    int32_t reserved;               /* 0                                                                 */
+    int64_t x_stride, q_stride;     /* >= width, below 2^30; q's % 16 == 0                               */
+    int64_t scale_stride;           /* >= blocks of 128, below 2^30                                      */
+} wpk_quantize_desc;
+
+int wpk_quantize_fwd(const wpk_quantize_desc *d, const void *x, void *q, float *scales, void *stream);
+
+/* y[i][j] = act(sum_k x[i][k] * w[j][k] + bias[j]) + residual[i][j] with x and w in 8 bits */
+typedef struct wpk_linear_q8_desc {
+    int32_t m, n, k;                /* as for wpk_linear_desc                                            */
+    int32_t dtype;                  /* of bias, residual and y: WPK_F32, WPK_BF16 or WPK_F16             */
+    int32_t act;                    /* WPK_ACT_*                                                         */
+    int32_t reserved;               /* 0                                                                 */
+    int64_t x_stride, w_stride;     /* elements between rows, >= k, % 16 == 0, below 2^20                */
+    int64_t y_stride, residual_stride;   /* >= n, below 2^20, also without a residual                    */
+    int64_t x_scale_stride, w_scale_stride;   /* >= blocks of 128 along k, below 2^20                     */
+} wpk_linear_q8_desc;
+
+/* Bytes of workspace that wpk_linear_q8_fwd needs for this descriptor (0: none), or a negative status.  Host only. */
+int64_t wpk_linear_q8_workspace_bytes(const wpk_linear_q8_desc *d);
+
+/* x [m][k] with x_scales [m][k/128], w [n][k] with w_scales [n/128][k/128] (block counts rounded up), bias [n] or NULL, residual
+ * [m][n] or NULL (may be y itself, with the same stride).  workspace as for wpk_linear_fwd. */
+int wpk_linear_q8_fwd(const wpk_linear_q8_desc *d, const void *x, const float *x_scales, const void *w, const float *w_scales,
+                      const void *bias, const void *residual, void *y, void *workspace, void *stream);
+
+/* Rows sorted by expert by their experts' weights: for the rows r = starts[g] .. starts[g+1]-1 of expert g
+ *   y[r][j] = act(x[source[r]] . w[g][j])                            plain; w is [groups][n][k]
+ *   y[r][j] = act(x[source[r]] . w[g][j]) * (x[source[r]] . w[g][n + j])    gated; w is [groups][2 n][k]
+ * without source x[r].  Rows of no expert are left alone.  In 8 bits a gated weight's halves have blocks of their own: w_scales is
+ * [groups][2][n/128][k/128]. */
+typedef struct wpk_grouped_linear_desc {
+    int32_t groups;                 /* experts, 1 .. 4096                                                */
+    int32_t rows;                   /* of y, all experts together (0 is allowed, 2^30 at most)           */
+    int32_t n, k;                   /* columns of y, reduction                                           */
+    int32_t x_rows;                 /* rows that x has; >= rows without source                           */
+    int32_t dtype;                  /* of x and w                                                        */
+    int32_t y_dtype;                /* dtype or WPK_F32; with WPK_E4M3: WPK_F32, WPK_BF16 or WPK_F16     */
+    int32_t act, gated;             /* WPK_ACT_*; 0 or 1                                                 */
+    int32_t reserved;               /* 0                                                                 */
+    int64_t x_stride, w_stride, y_stride;      /* elements between rows, >= k, k and n, below 2^20; x's and w's % 16 == 0 in 8 bits */
+    int64_t w_group_stride;         /* elements between experts' weights, >= a weight's rows * w_stride, below 2^40; % 16 == 0 in 8 bits */
+    int64_t x_scale_stride, w_scale_stride;    /* 8 bits: between rows of scales, >= blocks along k, below 2^20 */
+    int64_t w_scale_group_stride;   /* 8 bits: between experts' scales, >= their rows * w_scale_stride, below 2^40 */
+} wpk_grouped_linear_desc;
+
+/* Bytes of workspace that wpk_grouped_linear_fwd needs for this descriptor (0: none), or a negative status.  Host only. */
+int64_t wpk_grouped_linear_workspace_bytes(const wpk_grouped_linear_desc *d);
+
+/* starts: groups + 1 ascending int32 on the device, values outside 0 .. rows clamped to it, NULL with one expert, which then has
+ * all rows.  source: int32 [rows] on the device or NULL, values outside 0 .. x_rows-1 clamped to it.  x_scales and w_scales: NULL
+ * but in 8 bits. */
+int wpk_grouped_linear_fwd(const wpk_grouped_linear_desc *d, const void *x, const float *x_scales, const void *w,
+                           const float *w_scales, const int32_t *starts, const int32_t *source, void *y, void *workspace,
+                           void *stream);
+
+/* The router: for every token t
+ *   experts[t]    the k experts of the largest logits, largest first, the lower index first where they are equal; a NaN counts as
+ *                 -inf (and a negative zero as zero)
+ *   weights[t]    scale * exp(logit) over the sum of exp(logit), of the k chosen (normalize) or of all; zeros where the largest
+ *                 logit is -inf
+ * and the order that sorts the tokens by expert, tokens of one expert in their own order:
+ *   starts        expert e has the rows starts[e] .. starts[e+1]-1 of the sorted order
+ *   source[r]     the token of row r
+ *   place[t][j]   the row of token t's j-th expert
+ * These are wpk_grouped_linear_fwd's starts and source and, with weights, wpk_rms_norm_fwd's source and weights behind it. */
+typedef struct wpk_route_desc {
+    int32_t tokens, experts, k;     /* tokens (0 is allowed; tokens * k 2^30 at most), 1 .. 1024, 1 .. 32 and <= experts */
+    int32_t dtype;                  /* of logits: WPK_F32, WPK_BF16 or WPK_F16                           */
+    int32_t normalize;              /* 0 or 1                                                            */
+    float scale;
+    int64_t logits_stride;          /* >= experts, below 2^30                                            */
+} wpk_route_desc;
+
+/* Bytes of workspace that wpk_route_fwd needs for this descriptor (0: none), or a negative status.  Host only. */
+int64_t wpk_route_workspace_bytes(const wpk_route_desc *d);
+
+/* logits [tokens][experts]; experts, place int32 [tokens][k], weights fp32 [tokens][k], starts int32 [experts + 1], source int32
+ * [tokens * k].  starts, source and place may all be NULL (the choice alone).  workspace: 16-byte aligned, its contents before and
+ * after mean nothing. */
+int wpk_route_fwd(const wpk_route_desc *d, const void *logits, int32_t *experts, float *weights, int32_t *starts,
+                  int32_t *source, int32_t *place, void *workspace, void *stream);
 
 #ifdef __cplusplus
 }

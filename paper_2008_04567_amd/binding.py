@@ -13,7 +13,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("WPK_LIBRARY") or os.path.join(_HERE, "libwpk.so")
 N_GENES = 10
 NCHW, X_NHWC, Y_NHWC, NHWC = 0, 1, 2, 3   # layout codes of ConvDesc.layout
-F32, BF16, F16 = 0, 1, 2                  # element types
+F32, BF16, F16, E4M3 = 0, 1, 2, 3         # element types
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 
 (OK, E_BAD_DESC, E_NULL_PTR, E_UNSUPPORTED, E_HIP, E_NO_CONFIG, E_BAD_ARG, E_IO, E_VERIFY,
@@ -85,6 +85,36 @@ class SsmDesc(ctypes.Structure):
                                                "state_dim", "slots", "dtype", "dt_softplus")] +
                 [(f, ctypes.c_int64) for f in ("x_stride", "dt_stride", "b_stride", "c_stride", "z_stride",
                                                "y_stride")])
+
+
+class RmsNormDesc(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("rows", "width", "groups", "parts", "x_rows", "dtype")] +
+                [("eps", ctypes.c_float)] +
+                [(f, ctypes.c_int64) for f in ("x_stride", "residual_stride", "h_stride", "y_stride", "q_stride",
+                                               "scale_stride")])
+
+
+class QuantizeDesc(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("rows", "width", "dtype", "reserved")] +
+                [(f, ctypes.c_int64) for f in ("x_stride", "q_stride", "scale_stride")])
+
+
+class LinearQ8Desc(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("m", "n", "k", "dtype", "act", "reserved")] +
+                [(f, ctypes.c_int64) for f in ("x_stride", "w_stride", "y_stride", "residual_stride", "x_scale_stride",
+                                               "w_scale_stride")])
+
+
+class GroupedLinearDesc(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("groups", "rows", "n", "k", "x_rows", "dtype", "y_dtype", "act", "gated",
+                                               "reserved")] +
+                [(f, ctypes.c_int64) for f in ("x_stride", "w_stride", "y_stride", "w_group_stride", "x_scale_stride",
+                                               "w_scale_stride", "w_scale_group_stride")])
+
+
+class RouteDesc(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("tokens", "experts", "k", "dtype", "normalize")] +
+                [("scale", ctypes.c_float), ("logits_stride", ctypes.c_int64)])
 
 
 GA_CONSTRAINT_FN = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.POINTER(ctypes.c_int32), ctypes.c_int32,
@@ -183,6 +213,14 @@ def lib():
             "wpk_ssm_workspace_bytes": (ctypes.c_int64, [P(SsmDesc)]),
             "wpk_ssm_scan_fwd": (I, [P(SsmDesc)] + [V] * 16),
             "wpk_ssm_scan_step": (I, [P(SsmDesc)] + [V] * 13),
+            "wpk_rms_norm_fwd": (I, [P(RmsNormDesc)] + [V] * 10),
+            "wpk_quantize_fwd": (I, [P(QuantizeDesc)] + [V] * 4),
+            "wpk_linear_q8_workspace_bytes": (ctypes.c_int64, [P(LinearQ8Desc)]),
+            "wpk_linear_q8_fwd": (I, [P(LinearQ8Desc)] + [V] * 9),
+            "wpk_grouped_linear_workspace_bytes": (ctypes.c_int64, [P(GroupedLinearDesc)]),
+            "wpk_grouped_linear_fwd": (I, [P(GroupedLinearDesc)] + [V] * 9),
+            "wpk_route_workspace_bytes": (ctypes.c_int64, [P(RouteDesc)]),
+            "wpk_route_fwd": (I, [P(RouteDesc)] + [V] * 8),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -651,3 +689,105 @@ def ssm_scan_step(desc, x, dt, a, b, c, y, d=None, z=None, dt_bias=None, slot_ma
     _check(lib().wpk_ssm_scan_step(ctypes.byref(desc), _ptr(x), _ptr(dt), _ptr(a), _ptr(b), _ptr(c), _ptr(d),
                                    _ptr(z), _ptr(dt_bias), _ptr(slot_map), _ptr(state_in), _ptr(state_out), _ptr(y),
                                    _stream(stream)), "wpk_ssm_scan_step")
+
+
+# ---- around a mixer layer: normalisation, 8-bit products, experts ----------------------------------
+SCALE_BLOCK = 128         # values of a row, rows and columns of a weight, that share a scale in 8 bits
+
+
+def scale_blocks(width):
+    """Scales of a row of `width` 8-bit values."""
+    return -(-int(width) // SCALE_BLOCK)
+
+
+def make_rms_norm_desc(rows, width, groups=1, parts=1, x_rows=None, dtype=BF16, eps=1e-5, x_stride=None,
+                       residual_stride=None, h_stride=None, y_stride=None, q_stride=None, scale_stride=None):
+    """RmsNormDesc; strides default to dense rows (8-bit ones to multiples of 16), x_rows to rows * parts."""
+    pick = lambda v, default: int(default if v is None else v)
+    return RmsNormDesc(rows, width, groups, parts, pick(x_rows, rows * parts), dtype, eps, pick(x_stride, width),
+                       pick(residual_stride, width), pick(h_stride, width), pick(y_stride, width),
+                       pick(q_stride, -(-width // 16) * 16), pick(scale_stride, scale_blocks(width)))
+
+
+def rms_norm_fwd(desc, x, gain, y=None, q=None, scales=None, residual=None, h=None, source=None, weights=None,
+                 stream=None):
+    """s = residual + sum of the row's weighted parts; h = s; y and / or q with scales = s over its root mean square, times
+    gain."""
+    _check(lib().wpk_rms_norm_fwd(ctypes.byref(desc), _ptr(x), _ptr(source), _ptr(weights), _ptr(residual), _ptr(gain),
+                                  _ptr(h), _ptr(y), _ptr(q), _ptr(scales), _stream(stream)), "wpk_rms_norm_fwd")
+
+
+def make_quantize_desc(rows, width, dtype=BF16, x_stride=None, q_stride=None, scale_stride=None):
+    """QuantizeDesc; strides default to dense rows, 8-bit ones to multiples of 16."""
+    pick = lambda v, default: int(default if v is None else v)
+    return QuantizeDesc(rows, width, dtype, 0, pick(x_stride, width), pick(q_stride, -(-width // 16) * 16),
+                        pick(scale_stride, scale_blocks(width)))
+
+
+def quantize_fwd(desc, x, q, scales, stream=None):
+    """q, scales = x in 8 bits."""
+    _check(lib().wpk_quantize_fwd(ctypes.byref(desc), _ptr(x), _ptr(q), _ptr(scales), _stream(stream)),
+           "wpk_quantize_fwd")
+
+
+def make_linear_q8_desc(m, n, k, dtype=BF16, act=ACT_NONE, x_stride=None, w_stride=None, y_stride=None,
+                        residual_stride=None, x_scale_stride=None, w_scale_stride=None):
+    """LinearQ8Desc; strides default to dense rows, 8-bit ones to multiples of 16.  dtype is y's, bias's and residual's."""
+    pick = lambda v, default: int(default if v is None else v)
+    row, blocks = -(-k // 16) * 16, scale_blocks(k)
+    return LinearQ8Desc(m, n, k, dtype, act, 0, pick(x_stride, row), pick(w_stride, row), pick(y_stride, n),
+                        pick(residual_stride, n), pick(x_scale_stride, blocks), pick(w_scale_stride, blocks))
+
+
+def linear_q8_workspace(desc):
+    """Bytes of workspace that linear_q8_fwd needs for this descriptor."""
+    return _check(lib().wpk_linear_q8_workspace_bytes(ctypes.byref(desc)), "wpk_linear_q8_workspace_bytes")
+
+
+def linear_q8_fwd(desc, x, x_scales, w, w_scales, y, bias=None, residual=None, workspace=None, stream=None):
+    """y = act(x w^T + bias) + residual with x and w in 8 bits."""
+    _check(lib().wpk_linear_q8_fwd(ctypes.byref(desc), _ptr(x), _ptr(x_scales), _ptr(w), _ptr(w_scales), _ptr(bias),
+                                   _ptr(residual), _ptr(y), _ptr(workspace), _stream(stream)), "wpk_linear_q8_fwd")
+
+
+def make_grouped_linear_desc(groups, rows, n, k, dtype=BF16, y_dtype=None, act=ACT_NONE, gated=False, x_rows=None,
+                             x_stride=None, w_stride=None, y_stride=None, w_group_stride=None, x_scale_stride=None,
+                             w_scale_stride=None, w_scale_group_stride=None):
+    """GroupedLinearDesc; strides default to dense rows (8-bit ones to multiples of 16) and dense weights, x_rows to rows,
+    y_dtype to dtype, or bf16 for 8-bit rows."""
+    pick = lambda v, default: int(default if v is None else v)
+    row, blocks, halves = -(-k // 16) * 16 if dtype == E4M3 else k, scale_blocks(k), 2 if gated else 1
+    w_stride, w_scale_stride = pick(w_stride, row), pick(w_scale_stride, blocks)
+    return GroupedLinearDesc(groups, rows, n, k, pick(x_rows, rows), dtype, pick(y_dtype, BF16 if dtype == E4M3 else dtype),
+                             act, 1 if gated else 0, 0, pick(x_stride, row), w_stride, pick(y_stride, n),
+                             pick(w_group_stride, halves * n * w_stride), pick(x_scale_stride, blocks), w_scale_stride,
+                             pick(w_scale_group_stride, halves * scale_blocks(n) * w_scale_stride))
+
+
+def grouped_linear_workspace(desc):
+    """Bytes of workspace that grouped_linear_fwd needs for this descriptor."""
+    return _check(lib().wpk_grouped_linear_workspace_bytes(ctypes.byref(desc)), "wpk_grouped_linear_workspace_bytes")
+
+
+def grouped_linear_fwd(desc, x, w, starts, y, x_scales=None, w_scales=None, source=None, workspace=None, stream=None):
+    """Rows sorted by expert by their experts' weights, plain or gated."""
+    _check(lib().wpk_grouped_linear_fwd(ctypes.byref(desc), _ptr(x), _ptr(x_scales), _ptr(w), _ptr(w_scales), _ptr(starts),
+                                        _ptr(source), _ptr(y), _ptr(workspace), _stream(stream)),
+           "wpk_grouped_linear_fwd")
+
+
+def make_route_desc(tokens, experts, k, dtype=BF16, normalize=True, scale=1.0, logits_stride=None):
+    """RouteDesc; logits_stride defaults to dense rows."""
+    return RouteDesc(tokens, experts, k, dtype, 1 if normalize else 0, scale,
+                     int(experts if logits_stride is None else logits_stride))
+
+
+def route_workspace(desc):
+    """Bytes of workspace that route_fwd needs for this descriptor."""
+    return _check(lib().wpk_route_workspace_bytes(ctypes.byref(desc)), "wpk_route_workspace_bytes")
+
+
+def route_fwd(desc, logits, experts, weights, starts=None, source=None, place=None, workspace=None, stream=None):
+    """The experts of every token, their weights, and the order that sorts the tokens by expert."""
+    _check(lib().wpk_route_fwd(ctypes.byref(desc), _ptr(logits), _ptr(experts), _ptr(weights), _ptr(starts), _ptr(source),
+                               _ptr(place), _ptr(workspace), _stream(stream)), "wpk_route_fwd")

@@ -4,7 +4,7 @@
 ``build_library()``.  Translation units are compiled
 in parallel: the host part, the API/dispatch part, eight instantiation parts of the tiled
 kernel family, three of its split members, one of their strip form and one for each of the
-sequence layers' operators.  Works without a GPU (hipcc cross-compiles).
+sequence layers' and their surroundings' operators.  Works without a GPU (hipcc cross-compiles).
 """
 import concurrent.futures
 import os
@@ -17,7 +17,7 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libwpk.so")
 N_PARTS = 8
-SEQUENCE_PARTS = ("wpk_linear", "wpk_causal_conv", "wpk_ssm")
+SEQUENCE_PARTS = ("wpk_linear", "wpk_causal_conv", "wpk_ssm", "wpk_norm", "wpk_linear_q8", "wpk_grouped", "wpk_route")
 
 COMMON = ["-O3", "-fPIC", "-std=c++17", "-I" + INCLUDE, "-I" + CSRC, "-Wall", "-Wno-unused-function"]
 # packed-FP32 instructions are switched off for all device code
@@ -90,7 +90,7 @@ def build_library(force=True, verbose=False):
         headers + [src("wpk_igemm.h"), src("wpk_split.h"), src("wpk_strip.h"), src("wpk_strip_inst.hip")])
     for name in SEQUENCE_PARTS:
         add([hipcc] + COMMON + DEVICE + ["-c", src(name + ".hip"), "-o", os.path.join(OBJ, name + ".o")],
-            headers + [src("wpk_seq.h"), src("wpk_ssm_scan.h"), src(name + ".hip")])
+            headers + [src("wpk_seq.h"), src("wpk_ssm_scan.h"), src("wpk_product.h"), src("wpk_q8.h"), src(name + ".hip")])
     if jobs:
         workers = min(len(jobs), max(1, (os.cpu_count() or 4)), 16)
         with concurrent.futures.ThreadPoolExecutor(workers) as ex:
