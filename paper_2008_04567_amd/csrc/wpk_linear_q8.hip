@@ -62,17 +62,32 @@ template <int TM, int TN> struct StageSmall {
     }
 };
 
+// 4 bytes a lane from `rows` at the lane's `offset` plus `step` straight to LDS, as load_to_lds does with 16.
+__device__ inline void load_word_to_lds(Rows rows, uint32_t offset, uint32_t step, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n s_nop 0\n buffer_load_dword %0, %1, %3 offen lds"
+                 :
+                 : "v"(offset), "s"(rows), "s"(lds), "s"(step)
+                 : "m0", "memory");
+}
+
+typedef const __attribute__((address_space(4))) float *Constants;     // read by scalar loads
+
 // BM rows of y by BN rows of w, WM x WN waves.  Rows go to LDS directly, STAGES - 1 steps ahead, their 16-byte pieces in the
-// order of their number xor bits of the row's, so that 16 rows' same pieces take all banks.
+// order of their number xor bits of the row's, so that 16 rows' same pieces take all banks.  The scales of x go there too, eight
+// steps' at a time: a load a wave and step brings eight rows' for eight steps, the next eight steps' again and again until these
+// begin, so that the same number of loads is always under way.
 template <typename T, int BM, int BN, int WM, int WN, int STAGES, bool GROUPED, bool GATED>
-__global__ void __launch_bounds__(64 * WM * WN) linear_q8_kernel(Q8Args q)
+__global__ void __launch_bounds__(64 * WM * WN, (BM + BN) * 128 * STAGES > 73728 ? WM * WN / 4 : WM * WN / 2) linear_q8_kernel(Q8Args q)
 {
     typedef typename OperandFor<T>::type Operand;
     LinearArgs &a = q.a;
     const int kWaves = WM * WN, BK = 128, TM = BM / WM / 16, TN = BN / WN / 16, kOut = GATED ? BN / 2 : BN;
-    const int kPieces = 8, kLoadRows = 8, kLoads = (BM + BN) / kLoadRows / kWaves;
-    static_assert(BN / kLoadRows % kLoads == 0 && TM % 2 == 0 && TN % 2 == 0, "whole loads and blocks");
+    const int kPieces = 8, kLoadRows = 8, kLoads = (BM + BN) / kLoadRows / kWaves, kScaleLoads = BM / 8 / kWaves;
+    static_assert(BN / kLoadRows % kLoads == 0 && TM % 2 == 0 && TN % 2 == 0 && TM >= 4, "whole loads and blocks");
+    static_assert(BM % (8 * kWaves) == 0 && (kScaleLoads & (kScaleLoads - 1)) == 0 && kScaleLoads + STAGES <= 8, "whole loads of scales");
     __shared__ __align__(16) uint8_t lds[STAGES][(BM + BN) * BK];    // rows of w, then rows of x
+    __shared__ __align__(16) float scales[2][BM][8];
     static_assert(sizeof(lds) >= sizeof(float) * WM * WN * 32 * (16 * TN + 4), "what put_tile needs");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 15, g = lane >> 4;
     const int wm = wave % WM, wn = wave / WM, slice = GROUPED ? 0 : blockIdx.y;
@@ -107,20 +122,35 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_q8_kernel(Q8Args q)
         from[i] = (uint32_t)(row_at - base) * (uint32_t)stride + piece(i);
     }
     const uint32_t lds0 = lds_offset(&lds[0][0]) + wave * kLoads * 1024;
-    auto fetch = [&](int stage, int k) {
+    auto fetch = [&](int stage, int k, int first, int end) {
         const uint32_t to = lds0 + stage * (uint32_t)sizeof(lds[0]);
         const bool whole = k + BK <= k_end;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) load_to_lds(src, whole || k + piece(i) < k_end ? from[i] : kOutside, k, to + i * 1024);
+        for (int i = first; i < end; ++i) load_to_lds(src, whole || k + piece(i) < k_end ? from[i] : kOutside, k, to + i * 1024);
     };
 
-    const float *xs[TM];
+    // x's scales: this wave's rows, eight at a time, a step a lane
+    const int kb_begin = k_begin / BK, kb_end = (k_end + BK - 1) / BK;
+    const bool scales_far = GROUPED && a.source;
+    const Rows scale_src = __builtin_amdgcn_make_buffer_rsrc((float *)q.x_scales + (scales_far ? 0 : m0 * q.x_scale_stride), 0, 0x7fffffff, 0x00020000);
+    uint32_t scale_from[kScaleLoads];
 #pragma unroll
-    for (int i = 0; i < TM; ++i) xs[i] = q.x_scales + (int64_t)x_row<GROUPED>(a, m0 + (wm * TM + i) * 16 + row) * q.x_scale_stride;
+    for (int i = 0; i < kScaleLoads; ++i) {
+        const int r = x_row<GROUPED>(a, m0 + (wave * kScaleLoads + i) * 8 + lane / 8) - (scales_far ? 0 : m0);
+        scale_from[i] = (uint32_t)r * (uint32_t)q.x_scale_stride * 4u + lane % 8 * 4;
+    }
+    const uint32_t scales0 = lds_offset(&scales[0][0][0]) + wave * kScaleLoads * 256;
+    auto fetch_scales = [&](int run, int i) {                  // the i-th load of the steps 8 run .. 8 run + 7
+        uint32_t off = scale_from[0];
+#pragma unroll
+        for (int j = 1; j < kScaleLoads; ++j) off = i == j ? scale_from[j] : off;
+        const int kb = kb_begin + 8 * run;
+        load_word_to_lds(scale_src, kb + lane % 8 < kb_end ? off : kOutside, kb * 4, scales0 + (run & 1) * (uint32_t)sizeof(scales[0]) + i * 256);
+    };
     // (a wave's columns are of one block, or of one in each half)
-    const int block = (n0 + wn * TN * (GATED ? 8 : 16)) / kScaleBlock;
-    const float *const ws = q.w_scales + (int64_t)min(block, (a.n - 1) / kScaleBlock) * q.w_scale_stride;
-    const float *const ws_up = ws + (int64_t)((a.n + kScaleBlock - 1) / kScaleBlock) * q.w_scale_stride;
+    const int block = min((n0 + wn * TN * (GATED ? 8 : 16)) / kScaleBlock, (a.n - 1) / kScaleBlock);
+    const Constants ws = (Constants)(q.w_scales + (int64_t)block * q.w_scale_stride);
+    const Constants ws_up = (Constants)(q.w_scales + (int64_t)(block + (a.n + kScaleBlock - 1) / kScaleBlock) * q.w_scale_stride);
 
     f32x4 acc[TM][TN];
 #pragma unroll
@@ -128,78 +158,114 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_q8_kernel(Q8Args q)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
+    // What is behind a row's end in its last piece is not the row's.
+    auto clear_tail = [&](uint8_t *buf, int k) {
+        for (int r = tid; r < BM + BN; r += 64 * kWaves) {
+            u32x4 *const v = (u32x4 *)(buf + r * BK + (((k_end - k) / 16 ^ order(r)) * 16));
+            u32x4 u = *v;
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) fetch(s, k_begin + s * BK);
-    int stage = 0;
-    for (int k = k_begin; k < k_end; k += BK) {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * kLoads) : "memory");
-        __builtin_amdgcn_s_barrier();
-        fetch(stage == 0 ? STAGES - 1 : stage - 1, k + (STAGES - 1) * BK);
-        uint8_t *const buf = &lds[stage][0];
-        if (k + BK > k_end && k_end % 16 != 0) {               // what is behind a row's end in its last piece is not the row's
-            for (int r = tid; r < BM + BN; r += 64 * kWaves) {
-                const int p = (k_end - k) / 16;
-                u32x4 *const v = (u32x4 *)(buf + r * BK + ((p ^ order(r)) * 16));
-                u32x4 u = *v;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int left = min(max((k_end - k) % 16 - 4 * i, 0), 4);
-                    u[i] &= left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1;
-                }
-                *v = u;
+            for (int i = 0; i < 4; ++i) {
+                const int left = min(max((k_end - k) % 16 - 4 * i, 0), 4);
+                u[i] &= left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1;
             }
-            __syncthreads();
+            *v = u;
         }
-        auto read = [&](int r) {                               // row r of the tile, this lane's 32 entries
-            const uint8_t *const p = buf + r * BK;
-            const i32x4 lo = *(const i32x4 *)(p + ((2 * g) ^ order(r)) * 16), hi = *(const i32x4 *)(p + ((2 * g + 1) ^ order(r)) * 16);
-            return Operand::of(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        };
+        __syncthreads();
+    };
+    const int odd_k = k_end % 16 != 0 ? (k_end - k_begin) / BK * BK + k_begin : -1;      // the step that ends within a piece
+
+    uint32_t at_lo = row * BK + ((2 * g) ^ order(row)) * 16, at_hi = row * BK + ((2 * g + 1) ^ order(row)) * 16;
+    auto read = [&](const uint8_t *buf, int r) {               // row r + lane % 16 of a tile (r a multiple of 16), this lane's 32 entries
+        const i32x4 lo = *(const i32x4 *)(buf + r * BK + at_lo), hi = *(const i32x4 *)(buf + r * BK + at_hi);
+        return (i32x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    const int w_at = wn * TN * 16, x_at = BN + wm * TM * 16;
+
+    // A step's rows of x are read two ahead of the products, the first two and w's with the last products of the step before:
+    // between them all waves meet, the step's operands there and the buffer before it read by everyone.
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i) fetch_scales(0, i);
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s) {
+        if (s > 0) fetch_scales(0, 0);                         // (again, for the count)
+        fetch(s, k_begin + s * BK, 0, kLoads);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * (kLoads + 1)) : "memory");
+    __builtin_amdgcn_s_barrier();
+    if (odd_k == k_begin) clear_tail(&lds[0][0], k_begin);
+    i32x8 fw[TN], fx[2];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fw[j] = read(&lds[0][0], w_at + 16 * j);
+    fx[0] = read(&lds[0][0], x_at);
+    fx[1] = read(&lds[0][0], x_at + 16);
+    int stage = 0, step = 0;
+    for (int k = k_begin; k < k_end; k += BK, ++step) {
+        const int next = stage == STAGES - 1 ? 0 : stage + 1;
+        const uint8_t *const buf = &lds[stage][0];
+        uint8_t *const buf_next = &lds[next][0];
         const int kb = k / BK;
+        const float sw = ws[kb], su = GATED ? ws_up[kb] : sw;
         float sx[TM];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) sx[i] = xs[i][kb];
-        const float sw = ws[kb], su = GATED ? ws_up[kb] : sw;
-        Operand fw[TN];
+        for (int i = 0; i < TM; ++i) sx[i] = scales[step >> 3 & 1][wm * TM * 16 + i * 16 + row][step & 7];
+        f32x4 v[TN];
+        auto add = [&](int i, int j) {
+            const float s = sx[i] * (GATED && j % 2 ? su : sw);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) fw[j] = read(wn * TN * 16 + j * 16 + row);
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(v[j][r], s, acc[i][j][r]);
+            asm volatile("" : "+v"(acc[i][j]));                // (left to itself the compiler adds behind the branch below)
+        };
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            const Operand fx = read(BN + (wm * TM + i) * 16 + row);
+            if (i == TM - 2) {
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * (kLoads + 1)) : "memory");
+                __builtin_amdgcn_s_barrier();
+                if (k + BK == odd_k) clear_tail(buf_next, k + BK);
+                fetch_scales((step >> 3) + 1, step & (kScaleLoads - 1));
+                fetch(stage, k + STAGES * BK, 0, kLoads);
+            }
+            const Operand x = Operand::of(fx[i & 1]);
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
-                const f32x4 v = Operand::multiply(fw[j], fx);
-                const float s = sx[i] * (GATED && j % 2 ? su : sw);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(v[r], s, acc[i][j][r]);
+                if (i > 0) add(i - 1, j);
+                v[j] = Operand::multiply(Operand::of(fw[j]), x);
+                if (i == TM - 1) fw[j] = read(buf_next, w_at + 16 * j);
             }
+            fx[i & 1] = i < TM - 2 ? read(buf, x_at + 16 * (i + 2)) : read(buf_next, x_at + 16 * (i + 2 - TM));
+            __builtin_amdgcn_sched_barrier(0);
         }
-        stage = stage == STAGES - 1 ? 0 : stage + 1;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) add(TM - 1, j);
+        stage = next;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the loads of zeros write LDS too)
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");     // (the loads of zeros write LDS too)
     __syncthreads();
     float *const rows = (float *)&lds[0][0] + wave * 32 * (16 * TN + 4);
     put_tile<T, TM / 2, TN / 2, GROUPED, GATED>(a, StageSmall<TM, TN>{acc, rows}, rows, false, slice, k_begin, k_end, m0 + wm * TM * 16,
                                                 n0 + wn * TN * (GATED ? 8 : 16));
 }
 
-template <typename T> static int linear_q8_typed(const Q8Args &q, hipStream_t st)
+template <typename T, int B, int STAGES, bool GROUPED, bool GATED> static int launch_q8(const Q8Args &q, int64_t tiles, hipStream_t st)
 {
-    const LinearArgs &a = q.a;
-    const int64_t tiles = (int64_t)((a.m + 127) / 128) * ((a.n + 127) / 128);
     if (tiles * 512 >= 1ll << 32) return WPK_E_UNSUPPORTED;
-    hipLaunchKernelGGL((linear_q8_kernel<T, 128, 128, 2, 4, 4, false, false>), dim3((unsigned)tiles, a.slices), dim3(512), 0, st, q);
+    hipLaunchKernelGGL((linear_q8_kernel<T, B, B, 2, 4, STAGES, GROUPED, GATED>), dim3((unsigned)tiles, q.a.slices), dim3(512), 0, st, q);
     WPK_HIP(hipGetLastError());
     return WPK_OK;
 }
 
+template <typename T> static int linear_q8_typed(const Q8Args &q, hipStream_t st)
+{
+    auto tiles = [&](int64_t t) { return ((q.a.m + t - 1) / t) * ((q.a.n + t - 1) / t); };
+    if constexpr (sizeof(T) == 2)
+        if (tiles(256) >= kComputeUnits) return launch_q8<T, 256, 2, false, false>(q, tiles(256), st);
+    return launch_q8<T, 128, 4, false, false>(q, tiles(128), st);
+}
+
 template <typename T, bool GATED> static int grouped_q8_typed(const Q8Args &q, hipStream_t st)
 {
-    const GroupedGrid g(q.a, 128, GATED ? 64 : 128);
-    if (g.too_large(512)) return WPK_E_UNSUPPORTED;
-    hipLaunchKernelGGL((linear_q8_kernel<T, 128, 128, 2, 4, 4, true, GATED>), dim3(g.all), dim3(512), 0, st, q);
-    WPK_HIP(hipGetLastError());
-    return WPK_OK;
+    if constexpr (sizeof(T) == 2)
+        if (q.a.m / q.a.groups >= 256) return launch_q8<T, 256, 2, true, GATED>(q, GroupedGrid(q.a, 256, GATED ? 128 : 256).tiles, st);
+    return launch_q8<T, 128, 4, true, GATED>(q, GroupedGrid(q.a, 128, GATED ? 64 : 128).tiles, st);
 }
 
 int grouped_q8(const Q8Args &q, int y_dtype, bool gated, hipStream_t st)
