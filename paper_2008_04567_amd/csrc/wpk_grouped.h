@@ -16,15 +16,12 @@ struct Q8Args {
 // Workgroups for tiles of tile_m rows and tile_n columns of y of products by expert: as many as there could be.
 struct GroupedGrid {
     int64_t tiles;
-    unsigned all;
     GroupedGrid(const LinearArgs &a, int tile_m, int tile_n)
     {
         // (each expert has one tile at most that is not full)
         const int64_t tiles_m = ((int64_t)a.m + (int64_t)a.groups * (tile_m - 1)) / tile_m;
         tiles = (tiles_m < a.m ? tiles_m : a.m) * ((a.n + tile_n - 1) / tile_n);
-        all = (unsigned)tiles;
     }
-    bool too_large(int threads) const { return tiles * threads >= 1ll << 32; }
 };
 
 int grouped_q8(const Q8Args &q, int y_dtype, bool gated, hipStream_t st);

@@ -3,20 +3,65 @@
 
 namespace wpk {
 
-template <typename T, bool GATED> static int grouped_typed(const LinearArgs &a, bool direct, hipStream_t st)
+template <typename T, bool GATED> static int launch_grouped_rows(LinearArgs a, hipStream_t st)
 {
-    const GroupedGrid g(a, 64, GATED ? 32 : 64);
-    if (g.too_large(256)) return WPK_E_UNSUPPORTED;
-    if constexpr (sizeof(T) == 2) {
-        if (direct) {
-            hipLaunchKernelGGL((grouped_direct_kernel<T, 64, 64, 2, 2, 64, 4, GATED>), dim3(g.all), dim3(256), 0, st, a);
-            WPK_HIP(hipGetLastError());
-            return WPK_OK;
-        }
-    }
-    hipLaunchKernelGGL((grouped_tiles_kernel<T, 64, 64, 2, 2, GATED>), dim3(g.all), dim3(256), 0, st, a);
+    const int U = sizeof(T) == 2 ? 4 : 2;
+    a.width = GATED ? 16 : 32;
+    const GroupedGrid g(a, 16, a.width);
+    if (g.tiles * 64 * kRowsWaves >= 1ll << 32) return WPK_E_UNSUPPORTED;
+    hipLaunchKernelGGL((grouped_rows_kernel<T, 1, 2, U, GATED>), dim3((unsigned)g.tiles), dim3(64 * kRowsWaves), 0, st, a);
     WPK_HIP(hipGetLastError());
     return WPK_OK;
+}
+
+template <typename T, int B, int WM, int WN, int STAGES, bool GATED> static int launch_grouped_direct(const LinearArgs &a, hipStream_t st)
+{
+    const GroupedGrid g(a, B, GATED ? B / 2 : B);
+    if (g.tiles * 64 * WM * WN >= 1ll << 32) return WPK_E_UNSUPPORTED;
+    hipLaunchKernelGGL((grouped_direct_kernel<T, B, B, WM, WN, 64, STAGES, GATED>), dim3((unsigned)g.tiles), dim3(64 * WM * WN), 0, st, a);
+    WPK_HIP(hipGetLastError());
+    return WPK_OK;
+}
+
+template <typename T, int B, bool GATED> static int launch_grouped_tiles(const LinearArgs &a, hipStream_t st)
+{
+    const GroupedGrid g(a, B, GATED ? B / 2 : B);
+    if (g.tiles * 256 >= 1ll << 32) return WPK_E_UNSUPPORTED;
+    hipLaunchKernelGGL((grouped_tiles_kernel<T, B, B, 2, 2, GATED>), dim3((unsigned)g.tiles), dim3(256), 0, st, a);
+    WPK_HIP(hipGetLastError());
+    return WPK_OK;
+}
+
+// By the mean of the experts' rows and the workgroups there would be.  us, experts x columns x reduction (gated: twice the columns),
+// rows of uneven spread:
+//   bf16, rows kernel / tiles of 64 / 128 (two steps in LDS) / 256
+//     8 x 2048 x 2048           mean 1: 13 / 14 / 26 / 49      64: 61 / 24 / 36 / 59     256: - / 54 / 48 / 66    1024: - / 173 / 116 / 121
+//     64 x 1024 x 2048, gated   mean 4: 99 / 106 / 123 / 140   64: 453 / 148 / 152 / 192  128: 850 / 215 / 162 / 202   256: - / 359 / 242 / 216
+//     7 x 300 x 520             mean 95: 6.0 / 7.1 / 10
+//   (128 with four steps in LDS, for workgroups that have a compute unit to themselves: 8 x 2048 x 2048, mean 128, 26 against 37)
+//   fp32, rows kernel / tiles of 64 / 128
+//     8 x 2048 x 2048           mean 1: 28 / 89 / 157          32: 80 / 92 / 162         64: 119 / 94 / 162
+//     64 x 1024 x 2048, gated   mean 8: 222 / 294 / 402        16: 304 / 310 / 403      128: 1669 / 679 / 621
+//     128 x 768 x 1024, gated   mean 8: 205 / 223 / 313        16: 281 / 229 / 321
+//     7 x 300 x 520             mean 95: 10 / 24 / 48
+template <typename T, bool GATED> static int grouped_typed(const LinearArgs &a, bool direct, hipStream_t st)
+{
+    const int64_t rows = a.m, groups = a.groups, mean = rows / groups, out = GATED ? 16 : 32;
+    const int64_t few = ((groups < rows ? groups : rows) + rows / 16) * ((a.n + out - 1) / out);     // workgroups of the row kernel
+    auto columns = [&](int64_t b) { return GATED ? (a.n + b / 2 - 1) / (b / 2) : (a.n + b - 1) / b; };
+    if constexpr (sizeof(T) == 2) {
+        if (direct) {
+            if (few <= 2 * kComputeUnits) return launch_grouped_rows<T, GATED>(a, st);
+            if (mean >= 256 && rows / 256 * columns(256) >= kComputeUnits) return launch_grouped_direct<T, 256, 2, 4, 2, GATED>(a, st);
+            if (mean >= 96 && GroupedGrid(a, 128, GATED ? 64 : 128).tiles <= kComputeUnits)
+                return launch_grouped_direct<T, 128, 2, 4, 4, GATED>(a, st);
+            if (mean >= 96) return launch_grouped_direct<T, 128, 2, 4, 2, GATED>(a, st);
+            return launch_grouped_direct<T, 64, 2, 2, 4, GATED>(a, st);
+        }
+    }
+    if (mean <= 8 || few <= 6 * kComputeUnits) return launch_grouped_rows<T, GATED>(a, st);
+    if (mean >= 128 && rows / 128 * columns(128) >= 2 * kComputeUnits) return launch_grouped_tiles<T, 128, GATED>(a, st);
+    return launch_grouped_tiles<T, 64, GATED>(a, st);
 }
 
 static int check_grouped(const wpk_grouped_linear_desc *dp)

@@ -151,6 +151,14 @@ __device__ inline void group_rows(const LinearArgs &a, int g, int *first, int *l
 // where `id` is behind the last tile.  The number of tiles is known on the device alone: the grid has as many workgroups as there
 // could be, and those that have work are dealt out to the dies in equal runs, in which an expert's tiles of columns are next to
 // each other.  Every wave finds its tile by itself: two loads a lane for each 64 experts, and sums over lanes.
+// an address that all lanes have, where the compiler can see it
+template <typename P> __device__ inline P *uniform(P *p)
+{
+    const uint64_t v = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
+    return (P *)((uint64_t)hi << 32 | lo);
+}
+
 struct GroupTile {
     int n, group, row;                // which tile of columns, the expert, the tile's first row of y
 };
@@ -179,10 +187,10 @@ template <int ROWS> __device__ inline bool take_group_tile(LinearArgs &a, int id
             const int r0 = __builtin_amdgcn_readlane(first, of) + skip;
             out->group = g0 + of, out->row = r0;
             a.m = min(ROWS, __builtin_amdgcn_readlane(length, of) - skip);
-            a.w = (const char *)a.w + (g0 + of) * a.w_group_stride * (int64_t)elem;
-            a.y = (char *)a.y + r0 * a.y_stride * (int64_t)y_elem;
-            if (a.source) a.source += r0;
-            else a.x = (const char *)a.x + r0 * a.x_stride * (int64_t)elem;
+            a.w = uniform((const char *)a.w + (g0 + of) * a.w_group_stride * (int64_t)elem);
+            a.y = uniform((char *)a.y + r0 * a.y_stride * (int64_t)y_elem);
+            if (a.source) a.source = uniform(a.source + r0);
+            else a.x = uniform((const char *)a.x + r0 * a.x_stride * (int64_t)elem);
             return true;
         }
         before = __builtin_amdgcn_readlane(upto, 63);

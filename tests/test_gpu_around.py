@@ -499,3 +499,85 @@ def test_expert_layer_captured_and_on_two_streams(A, dtype8, tokens):
         torch.cuda.synchronize()
         for c, w in zip((first, second), want):
             assert all(torch.equal(a, b) for a, b in zip(c[1], w)), "replay %d" % turn
+
+
+# ---- every form that the rules choose between, with several whole steps and a rest ---------------------------
+def kernels_of(call):
+    """Names of the product kernels that a call launches."""
+    import torch
+    from torch.profiler import ProfilerActivity, profile
+    with profile(activities=[ProfilerActivity.CUDA]) as p:
+        call()
+        torch.cuda.synchronize()
+    return [e.name for e in p.events() if "linear_" in e.name or "grouped_" in e.name]
+
+
+def is_form(names, kernel, numbers):
+    """Whether a call's first kernel is `kernel` with these leading numbers among its template arguments."""
+    if not names:
+        pytest.skip("the profiler shows no kernels here")
+    # (some demanglers do not know the 16-bit types and lose the argument behind them)
+    tail = "".join("Li%dE" % v for v in numbers) if names[0].startswith("_Z") else ", ".join(str(v) for v in numbers[1:])
+    assert kernel in names[0] and tail in names[0], (kernel, numbers, names)
+
+
+Q8_FORMS = [("linear_q8_rows_kernel", (1, 1), "bf16", 3, 300, 5000, True), ("linear_q8_rows_kernel", (1, 2), "f16", 9, 5000, 2700, False),
+            ("linear_q8_rows_kernel", (1, 3), "f32", 16, 9000, 2200, False), ("linear_q8_rows_kernel", (2, 3), "bf16", 32, 8512, 2048, False),
+            ("linear_q8_rows_kernel", (2, 2), "f32", 20, 7000, 2500, False), ("linear_q8_rows_kernel", (4, 1), "bf16", 50, 2000, 1300, False),
+            ("linear_q8_rows_kernel", (4, 3), "f16", 64, 9000, 1500, False), ("linear_q8_kernel", (64, 128), "bf16", 70, 8512, 1111, False),
+            ("linear_q8_kernel", (64, 128), "f16", 130, 1030, 4100, True), ("linear_q8_kernel", (64, 128), "f32", 200, 1000, 8200, True),
+            ("linear_q8_kernel", (128, 128), "bf16", 2000, 3200, 4128, False), ("linear_q8_kernel", (128, 128), "f16", 1990, 3207, 4103, False),
+            ("linear_q8_kernel", (256, 256), "bf16", 4100, 4097, 1160, False), ("linear_q8_kernel", (256, 256), "f16", 4096, 4096, 1283, False)]
+
+
+@pytest.mark.parametrize("kernel,numbers,dtype,m,n,k,cut", Q8_FORMS)
+def test_linear_q8_forms(A, kernel, numbers, dtype, m, n, k, cut):
+    import torch
+    B, (code, ty) = A.B, A.TYPES[dtype][:2]
+    A.run_linear_q8(m, n, k, dtype, act="silu", pad=4)
+    desc = B.make_linear_q8_desc(m, n, k, dtype=code)
+    assert (B.linear_q8_workspace(desc) > 0) == cut
+    row = desc.x_stride
+    x, w = [torch.zeros((r, row), device="cuda", dtype=torch.uint8) for r in (m, n)]
+    xs, ws = torch.ones((m, B.scale_blocks(k)), device="cuda"), torch.ones((B.scale_blocks(n), B.scale_blocks(k)), device="cuda")
+    y, room = torch.empty((m, n), device="cuda", dtype=ty), A.workspace(B.linear_q8_workspace(desc))
+    names = kernels_of(lambda: B.linear_q8_fwd(desc, x, xs, w, ws, y, workspace=room))
+    is_form(names, kernel, numbers)
+    assert len(names) == (2 if cut else 1)
+
+
+GROUPED_FORMS = [("grouped_rows_kernel", (1, 2), "bf16", [1, 0, 3, 2], 200, 4200, True), ("grouped_rows_kernel", (1, 2), "f16", [5, 20, 0], 300, 2500, False),
+                 ("grouped_direct_kernel", (64, 64, 2, 2), "bf16", [60, 1, 90, 80], 2000, 520, False),
+                 ("grouped_direct_kernel", (64, 64, 2, 2), "f16", [60, 1, 90, 80], 1000, 456, True),
+                 ("grouped_direct_kernel", (128, 128, 2, 4, 64, 4), "bf16", [200, 130, 1, 120], 600, 712, True),
+                 ("grouped_direct_kernel", (128, 128, 2, 4, 64, 2), "f16", [200, 130, 1, 120], 6000, 264, False),
+                 ("grouped_direct_kernel", (128, 128, 2, 4, 64, 2), "bf16", [200, 130, 1, 120], 3000, 392, True),
+                 ("grouped_direct_kernel", (256, 256, 2, 4, 64, 2), "bf16", [900, 300, 0, 1200], 8000, 328, False),
+                 ("grouped_direct_kernel", (256, 256, 2, 4, 64, 2), "f16", [900, 300, 0, 1200], 4000, 200, True),
+                 ("grouped_rows_kernel", (1, 2), "f32", [3, 9, 0, 20], 500, 1300, True), ("grouped_rows_kernel", (1, 2), "f32", [60, 33, 1], 700, 700, False),
+                 ("grouped_tiles_kernel", (64, 64, 2, 2), "f32", [90, 100, 0, 120], 2300, 140, False),
+                 ("grouped_tiles_kernel", (64, 64, 2, 2), "bf16", [90, 100, 0, 120], 1300, 141, True),
+                 ("grouped_tiles_kernel", (128, 128, 2, 2), "f32", [400, 300, 1, 500], 4000, 200, True),
+                 ("grouped_tiles_kernel", (128, 128, 2, 2), "f16", [400, 300, 1, 500], 8000, 133, False),
+                 ("linear_q8_rows_kernel", (1, 2), "e4m3", [1, 0, 17, 2], 300, 2900, True), ("linear_q8_rows_kernel", (1, 2), "e4m3", [5, 20, 0], 900, 5000, False),
+                 ("linear_q8_kernel", (64, 128), "e4m3", [60, 1, 90, 80], 3000, 700, True), ("linear_q8_kernel", (64, 128), "e4m3", [100, 0, 200], 3000, 1100, False),
+                 ("linear_q8_kernel", (128, 128), "e4m3", [900, 300, 0, 1200], 3600, 1040, False), ("linear_q8_kernel", (128, 128), "e4m3", [900, 300, 0, 1100], 1900, 1111, True),
+                 ("linear_q8_kernel", (256, 256), "e4m3", [1500, 900, 0, 1700], 8200, 1036, False), ("linear_q8_kernel", (256, 256), "e4m3", [1500, 900, 0, 1700], 4400, 1040, True)]
+
+
+@pytest.mark.parametrize("kernel,numbers,dtype,lengths,n,k,gated", GROUPED_FORMS)
+def test_grouped_forms(A, kernel, numbers, dtype, lengths, n, k, gated):
+    import torch
+    B, rows, groups, halves = A.B, sum(lengths), len(lengths), 2 if gated else 1
+    A.run_grouped(lengths, n, k, dtype, act="silu", gated=gated, gather=len(lengths) == 4)
+    code = B.E4M3 if dtype == "e4m3" else A.TYPES[dtype][0]
+    desc = B.make_grouped_linear_desc(groups, rows, n, k, dtype=code, gated=gated)
+    ty = torch.uint8 if dtype == "e4m3" else A.TYPES[dtype][1]
+    x, w = torch.zeros((rows, desc.x_stride), device="cuda", dtype=ty), torch.zeros((groups, halves * n, desc.w_stride), device="cuda", dtype=ty)
+    y = torch.empty((rows, n), device="cuda", dtype=torch.bfloat16 if dtype == "e4m3" else ty)
+    kw = dict(x_scales=torch.ones((rows, B.scale_blocks(k)), device="cuda"),
+              w_scales=torch.ones((groups, halves, B.scale_blocks(n), B.scale_blocks(k)), device="cuda")) if dtype == "e4m3" else {}
+    starts = A.i32([0] + np.cumsum(lengths).tolist())
+    names = kernels_of(lambda: B.grouped_linear_fwd(desc, x, w, starts, y, **kw))
+    is_form(names, kernel, numbers)
+    assert len(names) == 1
