@@ -26,6 +26,9 @@ __device__ inline float wave_sum(float v)
     return v;
 }
 
+// the number of this workgroup, in a grid of two dimensions
+__device__ inline int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // LANES lanes to a row (of one group), P pieces of eight elements each lane; a workgroup of 256 threads has several rows where
 // LANES is 64.  ALL: a row is LANES * P * 8 elements exactly.
 template <typename T, int LANES, int P, bool ALL> __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) rms_norm_kernel(NormArgs a)
@@ -33,11 +36,11 @@ template <typename T, int LANES, int P, bool ALL> __global__ void __launch_bound
     const int kWaves = LANES / 64;
     const int lane = threadIdx.x % LANES;
     const int64_t units = (int64_t)a.rows * a.groups;
-    int64_t unit = blockIdx.x;
+    int64_t unit = workgroup();
     if (LANES == 64) {
         unit = unit * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (unit >= units) return;
     }
+    if (unit >= units) return;
     const int64_t row = a.groups == 1 ? unit : unit / a.groups;
     const int c0 = a.groups == 1 ? 0 : (int)(unit - row * a.groups) * a.width;
 
@@ -129,7 +132,7 @@ template <typename T, int U> __global__ void __launch_bounds__(256) quantize_ker
 {
     const int unit = threadIdx.x >> 4, lane = threadIdx.x & 15, rows = 16 >> a.shift;
     const int in_row = unit & ((1 << a.shift) - 1);
-    const int64_t row0 = (int64_t)blockIdx.x * (a.shift == 4 ? 1 : rows * U) + (unit >> a.shift);
+    const int64_t row0 = workgroup() * (a.shift == 4 ? 1 : rows * U) + (unit >> a.shift);
     // either U rows of up to 16 blocks, or one row U times 16 blocks at a time
     for (int b0 = 0; b0 < a.blocks; b0 += 16 * U) {
         f32x8 v[U];
@@ -158,10 +161,13 @@ static bool stride_ok(int64_t stride, int64_t least, int64_t most, int *rc)
     return *rc == WPK_OK;
 }
 
+// Workgroups `n` in two dimensions, since threads in one are fewer than 2^32.
+static dim3 grid_of(int64_t n) { return n <= 1 << 20 ? dim3((unsigned)n) : dim3(1 << 20, (unsigned)((n + (1 << 20) - 1) >> 20)); }
+
 template <typename T, int LANES, int P> static void launch_norm(const NormArgs &a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.rows * a.groups;
-    const dim3 grid((unsigned)(LANES == 64 ? (units + 3) / 4 : units)), block(LANES < 256 ? 256 : LANES);
+    const dim3 grid = grid_of(LANES == 64 ? (units + 3) / 4 : units), block(LANES < 256 ? 256 : LANES);
     if (a.width == LANES * P * 8) hipLaunchKernelGGL((rms_norm_kernel<T, LANES, P, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((rms_norm_kernel<T, LANES, P, false>), grid, block, 0, st, a);
 }
@@ -181,13 +187,19 @@ template <typename T> static int norm_typed(const NormArgs &a, hipStream_t st)
     return WPK_OK;
 }
 
-template <typename T> static int quantize_typed(const QuantizeArgs &a, hipStream_t st)
+template <typename T, int U> static int launch_quantize(const QuantizeArgs &a, hipStream_t st)
 {
-    const int U = 4;
     const int64_t rows = a.shift == 4 ? 1 : (int64_t)(16 >> a.shift) * U;
-    hipLaunchKernelGGL((quantize_kernel<T, U>), dim3((unsigned)((a.rows + rows - 1) / rows)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((quantize_kernel<T, U>), grid_of((a.rows + rows - 1) / rows), dim3(256), 0, st, a);
     WPK_HIP(hipGetLastError());
     return WPK_OK;
+}
+
+template <typename T> static int quantize_typed(const QuantizeArgs &a, hipStream_t st)
+{
+    if (a.shift == 4 && a.blocks <= 16) return launch_quantize<T, 1>(a, st);
+    if (a.shift == 4 && a.blocks <= 32) return launch_quantize<T, 2>(a, st);
+    return launch_quantize<T, 4>(a, st);
 }
 
 }  // namespace wpk
