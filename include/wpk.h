@@ -542,7 +542,7 @@ int wpk_ssm_scan_step(const wpk_ssm_desc *d, const void *x, const void *dt, cons
  * 8 bits.  A row of e4m3 values q has one fp32 scale for each 128 of them, rows of scales `*_scale_stride` elements apart: the row
  * stands for q[c] * scale[c / 128].  The last block may be shorter.  A weight has one scale for each block of 128 rows and 128
  * columns: row j stands for q[j][c] * scale[j / 128][c / 128].  Rows of 8-bit values start at multiples of 16 bytes (pointers and
- * strides); what is behind a row's values, up to the next multiple of 16, is not used and not written.
+ * strides) and have room up to the next one; what is there behind a row's values may be read, is not used, and is not written.
  * From a row v in 32 bits they are made so: scale = max |v| of the block / 448, at least 2^-110, inverse = 1 / scale, q = v * inverse
  * rounded to the nearest e4m3 number, ties to even, none beyond 448.  A NaN stays one and leaves the rest of its block alone; a
  * block with an infinity has an infinite scale, and no value of it means a number.
@@ -568,8 +568,8 @@ typedef struct wpk_rms_norm_desc {
 } wpk_rms_norm_desc;
 
 /* x [x_rows][width], source int32 [rows][parts] or NULL, weights fp32 [rows][parts] or NULL, residual [rows][width] or NULL,
- * gain [width] or NULL (all ones); h, y, q with scales: any of them NULL, not all.  h may be the residual itself, y or h x
- * itself where parts is 1 and source NULL, y the residual or h no other (same stride for what is the same). */
+ * gain [width] or NULL (all ones); h, y, q with scales: any of them NULL, not all.  h may be the residual itself, and y
+ * may be x itself where parts is 1 and source NULL, each with the same stride; otherwise outputs may not overlap inputs. */
 int wpk_rms_norm_fwd(const wpk_rms_norm_desc *d, const void *x, const int32_t *source, const float *weights,
                      const void *residual, const void *gain, void *h, void *y, void *q, float *scales, void *stream);
 
@@ -606,7 +606,8 @@ int wpk_linear_q8_fwd(const wpk_linear_q8_desc *d, const void *x, const float *x
 /* Rows sorted by expert by their experts' weights: for the rows r = starts[g] .. starts[g+1]-1 of expert g
  *   y[r][j] = act(x[source[r]] . w[g][j])                            plain; w is [groups][n][k]
  *   y[r][j] = act(x[source[r]] . w[g][j]) * (x[source[r]] . w[g][n + j])    gated; w is [groups][2 n][k]
- * without source x[r].  Rows of no expert are left alone.  In 8 bits a gated weight's halves have blocks of their own: w_scales is
+ * without source x[r].  Rows of no expert are left alone.  A call that looks rows up in more than 2^31 bytes of 8-bit values, or of
+ * their scales, or has 8-bit gated weights of as many an expert, is refused (WPK_E_UNSUPPORTED).  In 8 bits a gated weight's halves have blocks of their own: w_scales is
  * [groups][2][n/128][k/128]. */
 typedef struct wpk_grouped_linear_desc {
     int32_t groups;                 /* experts, 1 .. 4096                                                */

@@ -530,7 +530,7 @@ int grouped_q8(const Q8Args &q, int y_dtype, bool gated, hipStream_t st)
 {
     // Loads reach 2^31 bytes from the first row where rows are looked up or a weight has two halves.
     const int64_t far = 1ll << 31;
-    if ((q.a.source && q.a.x_rows * q.a.x_stride >= far) || (gated && 2ll * q.a.n * q.a.w_stride >= far)) return WPK_E_UNSUPPORTED;
+    if ((q.a.source && (q.a.x_rows * q.a.x_stride >= far || q.a.x_rows * q.x_scale_stride * 4 >= far)) || (gated && 2ll * q.a.n * q.a.w_stride >= far)) return WPK_E_UNSUPPORTED;
     if (y_dtype == WPK_BF16) return gated ? grouped_q8_typed<bf16, true>(q, st) : grouped_q8_typed<bf16, false>(q, st);
     if (y_dtype == WPK_F16) return gated ? grouped_q8_typed<f16, true>(q, st) : grouped_q8_typed<f16, false>(q, st);
     return gated ? grouped_q8_typed<float, true>(q, st) : grouped_q8_typed<float, false>(q, st);

@@ -31,7 +31,7 @@ __device__ inline int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x +
 
 // LANES lanes to a row (of one group), P pieces of eight elements each lane; a workgroup of 256 threads has several rows where
 // LANES is 64.  ALL: a row is LANES * P * 8 elements exactly.
-template <typename T, int LANES, int P, bool ALL> __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) rms_norm_kernel(NormArgs a)
+template <typename T, int LANES, int P, bool ALL, bool FAR> __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) rms_norm_kernel(NormArgs a)
 {
     const int kWaves = LANES / 64;
     const int lane = threadIdx.x % LANES;
@@ -55,13 +55,13 @@ template <typename T, int LANES, int P, bool ALL> __global__ void __launch_bound
     auto row_of = [&](const void *base, int64_t stride, int64_t r, int p) { return (const T *)base + r * stride + at[p]; };
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        if (a.residual) s[p] = Eight<T>::template load<ALL>(row_of(a.residual, a.residual_stride, row, p), left[p]);
+        if (a.residual) s[p] = Eight<T>::template load<ALL, false>(row_of(a.residual, a.residual_stride, row, p), left[p]);
         else s[p] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
     }
     if (a.parts == 1 && !a.source) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            f32x8 v = Eight<T>::template load<ALL>(row_of(a.x, a.x_stride, row, p), left[p]);
+            f32x8 v = Eight<T>::template load<ALL, FAR>(row_of(a.x, a.x_stride, row, p), left[p]);
             if (a.weights) v *= a.weights[row];
             s[p] += v;
         }
@@ -78,7 +78,7 @@ template <typename T, int LANES, int P, bool ALL> __global__ void __launch_bound
                 w[j] = there ? (a.weights ? a.weights[e] : 1.0f) : 0.0f;
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
-                    v[j][p] = Eight<T>::template load<ALL>(row_of(a.x, a.x_stride, there ? from : 0, p), left[p]);
+                    v[j][p] = Eight<T>::template load<ALL, FAR>(row_of(a.x, a.x_stride, there ? from : 0, p), left[p]);
                     if (!there) v[j][p] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
                 }
             }
@@ -90,7 +90,7 @@ template <typename T, int LANES, int P, bool ALL> __global__ void __launch_bound
     }
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        if (a.gain) gain[p] = Eight<T>::template load<ALL>((const T *)a.gain + at[p], left[p]);
+        if (a.gain) gain[p] = Eight<T>::template load<ALL, false>((const T *)a.gain + at[p], left[p]);
         else gain[p] = f32x8{1, 1, 1, 1, 1, 1, 1, 1};
     }
     float sum = 0.0f;
@@ -98,7 +98,7 @@ template <typename T, int LANES, int P, bool ALL> __global__ void __launch_bound
     for (int p = 0; p < P; ++p) {
         const f32x8 e = s[p] * s[p];
         sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-        if (a.h && (ALL || left[p] > 0)) Eight<T>::template store<ALL>((T *)a.h + row * a.h_stride + at[p], left[p], s[p]);
+        if (a.h && (ALL || left[p] > 0)) Eight<T>::template store<ALL, FAR>((T *)a.h + row * a.h_stride + at[p], left[p], s[p]);
     }
     sum = wave_sum(sum);
     if (kWaves > 1) {
@@ -113,9 +113,9 @@ template <typename T, int LANES, int P, bool ALL> __global__ void __launch_bound
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         const f32x8 v = s[p] * r * gain[p];
-        if (a.y && (ALL || left[p] > 0)) Eight<T>::template store<ALL>((T *)a.y + row * a.y_stride + at[p], left[p], v);
+        if (a.y && (ALL || left[p] > 0)) Eight<T>::template store<ALL, FAR>((T *)a.y + row * a.y_stride + at[p], left[p], v);
         // (a row's last block: the lanes behind it hold zeros)
-        if (a.q) store_8<ALL>(a.q + row * a.q_stride + at[p], a.scales + row * a.scale_stride + at[p] / kScaleBlock, left[p], v, lane % 16 == 0);
+        if (a.q) store_8<ALL, FAR>(a.q + row * a.q_stride + at[p], a.scales + row * a.scale_stride + at[p] / kScaleBlock, left[p], v, lane % 16 == 0);
     }
 }
 
@@ -128,7 +128,7 @@ struct QuantizeArgs {
 };
 
 // 16 lanes to a block, U blocks a lane under way.
-template <typename T, int U> __global__ void __launch_bounds__(256) quantize_kernel(QuantizeArgs a)
+template <typename T, int U, bool FAR> __global__ void __launch_bounds__(256) quantize_kernel(QuantizeArgs a)
 {
     const int unit = threadIdx.x >> 4, lane = threadIdx.x & 15, rows = 16 >> a.shift;
     const int in_row = unit & ((1 << a.shift) - 1);
@@ -144,11 +144,11 @@ template <typename T, int U> __global__ void __launch_bounds__(256) quantize_ker
             c[u] = ((int64_t)(a.shift == 4 ? b0 + 16 * u : 0) + in_row) * kScaleBlock + lane * 8;
             left[u] = row[u] < a.rows && c[u] < a.width ? (int)min((int64_t)a.width - c[u], (int64_t)8) : 0;
             v[u] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
-            if (left[u] > 0) v[u] = Eight<T>::template load<false>((const T *)a.x + row[u] * a.x_stride + c[u], left[u]);
+            if (left[u] > 0) v[u] = Eight<T>::template load<false, FAR>((const T *)a.x + row[u] * a.x_stride + c[u], left[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            store_8<false>(a.q + row[u] * a.q_stride + c[u], a.scales + row[u] * a.scale_stride + c[u] / kScaleBlock, left[u], v[u],
+            store_8<false, FAR>(a.q + row[u] * a.q_stride + c[u], a.scales + row[u] * a.scale_stride + c[u] / kScaleBlock, left[u], v[u],
                            lane == 0);
         if (a.shift < 4) break;
     }
@@ -168,8 +168,11 @@ template <typename T, int LANES, int P> static void launch_norm(const NormArgs &
 {
     const int64_t units = (int64_t)a.rows * a.groups;
     const dim3 grid = grid_of(LANES == 64 ? (units + 3) / 4 : units), block(LANES < 256 ? 256 : LANES);
-    if (a.width == LANES * P * 8) hipLaunchKernelGGL((rms_norm_kernel<T, LANES, P, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((rms_norm_kernel<T, LANES, P, false>), grid, block, 0, st, a);
+    const bool all = a.width == LANES * P * 8, far = units * a.width * (a.parts + 1) * (int64_t)sizeof(T) > kFarBytes;
+    if (all && far) hipLaunchKernelGGL((rms_norm_kernel<T, LANES, P, true, true>), grid, block, 0, st, a);
+    else if (all) hipLaunchKernelGGL((rms_norm_kernel<T, LANES, P, true, false>), grid, block, 0, st, a);
+    else if (far) hipLaunchKernelGGL((rms_norm_kernel<T, LANES, P, false, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((rms_norm_kernel<T, LANES, P, false, false>), grid, block, 0, st, a);
 }
 
 template <typename T> static int norm_typed(const NormArgs &a, hipStream_t st)
@@ -190,7 +193,9 @@ template <typename T> static int norm_typed(const NormArgs &a, hipStream_t st)
 template <typename T, int U> static int launch_quantize(const QuantizeArgs &a, hipStream_t st)
 {
     const int64_t rows = a.shift == 4 ? 1 : (int64_t)(16 >> a.shift) * U;
-    hipLaunchKernelGGL((quantize_kernel<T, U>), grid_of((a.rows + rows - 1) / rows), dim3(256), 0, st, a);
+    const dim3 grid = grid_of((a.rows + rows - 1) / rows);
+    if ((int64_t)a.rows * a.width * (int64_t)sizeof(T) > kFarBytes) hipLaunchKernelGGL((quantize_kernel<T, U, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((quantize_kernel<T, U, false>), grid, dim3(256), 0, st, a);
     WPK_HIP(hipGetLastError());
     return WPK_OK;
 }

@@ -4,8 +4,8 @@
 
 ``Mixer`` owns the weights and a pool of states (one entry per request: the convolution's last inputs and the scan's
 state); ``prompt`` takes the ragged prompts of some requests, ``step`` one token of each.  Tensors and streams are
-PyTorch's; every operation is the library's.  An example: its weights are random, and it is the four calls alone, without
-the normalisations that models put around and into such a layer.
+PyTorch's; every operation is the library's.  An example: its weights are random.  Without ``norm`` it is the four calls alone; with
+it h goes through an RMS norm before the first product, and the scan's rows through one of as many groups before the last.
 
 What a call returns is the plan's own buffer: it holds until the plan's next call.  A plan's calls share buffers and
 workspace, so they belong on one stream, or in order; so do calls of any plans that use the same entries of the pool.
@@ -25,7 +25,7 @@ _CODES = {torch.float32: B.F32, torch.bfloat16: B.BF16, torch.float16: B.F16}
 
 class Mixer:
     def __init__(self, width, heads, head_dim, groups, state_dim, conv_width=4, slots=64, dtype=torch.bfloat16, seed=0,
-                 device="cuda"):
+                 device="cuda", norm=False):
         self.width, self.heads, self.head_dim = width, heads, head_dim
         self.groups, self.state_dim, self.conv_width, self.slots = groups, state_dim, conv_width, slots
         self.dtype, self.code, self.device = dtype, _CODES[dtype], device
@@ -42,6 +42,8 @@ class Mixer:
         d0 = torch.exp(math.log(1e-3) + math.log(100.0) * torch.rand(heads, generator=g, device=device))
         self.dt_bias = d0 + torch.log(-torch.expm1(-d0))
         self.d = torch.ones(heads, device=device)
+        self.norm = norm
+        self.gain_in, self.gain_out = torch.ones(width, device=device, dtype=dtype), torch.ones(self.inner, device=device, dtype=dtype)
         self.conv_state = torch.zeros((slots, conv_width - 1, self.conv_channels), device=device, dtype=dtype)
         self.scan_state = torch.zeros((slots, heads, head_dim, state_dim), device=device)
 
@@ -104,14 +106,22 @@ class _Plan:
         self.ssm_desc = B.make_ssm_desc(sequences, tokens, m.heads, m.head_dim, m.groups, m.state_dim, max_length=max_length,
                                         slots=m.slots, dtype=m.code, dt_softplus=True, x_stride=m.conv_channels,
                                         b_stride=m.conv_channels, c_stride=m.conv_channels, z_stride=m.row, dt_stride=m.row)
+        self.normed = empty(tokens, m.width) if m.norm else None
+        self.norm_in = B.make_rms_norm_desc(tokens, m.width, dtype=m.code)
+        self.norm_out = B.make_rms_norm_desc(tokens, inner, groups=m.groups, dtype=m.code)
         need = max(B.linear_workspace(self.lin_in), B.linear_workspace(self.lin_out), B.ssm_workspace(self.ssm_desc))
         self.workspace = torch.empty(max(16, need), device=m.device, dtype=torch.uint8)
 
     def run(self, h, starts, slot_map, resume, step, stream):
         m = self.m
         s = stream if stream is not None else torch.cuda.current_stream()
-        self.lin_in.x_stride = self.lin_out.residual_stride = h.stride(0) if self.tokens > 1 else m.width
-        B.linear_fwd(self.lin_in, h, m.w_in, self.row, workspace=self.workspace, stream=s)
+        row, x = h.stride(0) if self.tokens > 1 else m.width, h
+        self.lin_in.x_stride = self.lin_out.residual_stride = self.norm_in.x_stride = row
+        if m.norm:
+            x = self.normed
+            self.lin_in.x_stride = m.width
+            B.rms_norm_fwd(self.norm_in, h, m.gain_in, y=x, stream=s)
+        B.linear_fwd(self.lin_in, x, m.w_in, self.row, workspace=self.workspace, stream=s)
         conv = dict(bias=m.b_conv, slot_map=slot_map, state_in=m.conv_state, state_out=m.conv_state, stream=s)
         scan = dict(d=m.d, z=self.z, dt_bias=m.dt_bias, slot_map=slot_map, state_in=m.scan_state, state_out=m.scan_state,
                     stream=s)
@@ -122,6 +132,8 @@ class _Plan:
             B.causal_conv1d_fwd(self.conv_desc, self.xbc, m.w_conv, self.conv, starts=starts, resume=resume, **conv)
             B.ssm_scan_fwd(self.ssm_desc, self.x, self.dt, m.a, self.b, self.c, self.y, starts=starts, resume=resume,
                            workspace=self.workspace, **scan)
+        if m.norm:
+            B.rms_norm_fwd(self.norm_out, self.y, m.gain_out, y=self.y, stream=s)
         B.linear_fwd(self.lin_out, self.y, m.w_out, self.out, residual=h, workspace=self.workspace, stream=s)
         return self.out
 

@@ -581,3 +581,12 @@ def test_grouped_forms(A, kernel, numbers, dtype, lengths, n, k, gated):
     names = kernels_of(lambda: B.grouped_linear_fwd(desc, x, w, starts, y, **kw))
     is_form(names, kernel, numbers)
     assert len(names) == 1
+
+
+# ---- passes over more bytes than the caches hold take another form -------------------------------------------
+def test_norm_and_quantize_of_many_bytes(A):
+    A.run_norm(4100, 2048, "f32", q=True)
+    A.run_norm(4100, 2050, "f32", q=True, pad=1, offset=1)
+    A.run_norm(2100, 1024, "bf16", parts=17, source="random", weights="random")
+    eight(A, A.Rng(1).normal((8200, 2050)))
+    eight(A, A.Rng(2).normal((270000, 130), "bf16"), pad=1, offset=1)
