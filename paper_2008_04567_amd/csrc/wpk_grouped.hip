@@ -37,12 +37,15 @@ template <typename T, int B, bool GATED> static int launch_grouped_tiles(const L
 //   bf16, rows kernel / tiles of 64 / 128 (two steps in LDS) / 256
 //     8 x 2048 x 2048           mean 1: 13 / 14 / 26 / 49      64: 61 / 24 / 36 / 59     256: - / 54 / 48 / 66    1024: - / 173 / 116 / 121
 //     64 x 1024 x 2048, gated   mean 4: 99 / 106 / 123 / 140   64: 453 / 148 / 152 / 192  128: 850 / 215 / 162 / 202   256: - / 359 / 242 / 216
+//     64 x 2048 x 1536          mean 4: 86 / 77               64 x 2048 x 1024           mean 4: 62 / 57
+//     16 x 4096 x 4096          mean 1: 60 / 77               4: 92 / 101
 //     7 x 300 x 520             mean 95: 6.0 / 7.1 / 10
 //   (128 with four steps in LDS, for workgroups that have a compute unit to themselves: 8 x 2048 x 2048, mean 128, 26 against 37)
 //   fp32, rows kernel / tiles of 64 / 128
 //     8 x 2048 x 2048           mean 1: 28 / 89 / 157          32: 80 / 92 / 162         64: 119 / 94 / 162
 //     64 x 1024 x 2048, gated   mean 8: 222 / 294 / 402        16: 304 / 310 / 403      128: 1669 / 679 / 621
 //     128 x 768 x 1024, gated   mean 8: 205 / 223 / 313        16: 281 / 229 / 321
+//     16 x 2008 x 1024          mean 13: 47 / 54              20: 57 / 55               30: 76 / 55
 //     7 x 300 x 520             mean 95: 10 / 24 / 48
 template <typename T, bool GATED> static int grouped_typed(const LinearArgs &a, bool direct, hipStream_t st)
 {
@@ -51,7 +54,7 @@ template <typename T, bool GATED> static int grouped_typed(const LinearArgs &a, 
     auto columns = [&](int64_t b) { return GATED ? (a.n + b / 2 - 1) / (b / 2) : (a.n + b - 1) / b; };
     if constexpr (sizeof(T) == 2) {
         if (direct) {
-            if (few <= 2 * kComputeUnits) return launch_grouped_rows<T, GATED>(a, st);
+            if (few <= 2 * kComputeUnits || (mean <= 4 && a.k >= 2048)) return launch_grouped_rows<T, GATED>(a, st);
             if (mean >= 256 && rows / 256 * columns(256) >= kComputeUnits) return launch_grouped_direct<T, 256, 2, 4, 2, GATED>(a, st);
             if (mean >= 96 && GroupedGrid(a, 128, GATED ? 64 : 128).tiles <= kComputeUnits)
                 return launch_grouped_direct<T, 128, 2, 4, 4, GATED>(a, st);
@@ -59,7 +62,7 @@ template <typename T, bool GATED> static int grouped_typed(const LinearArgs &a, 
             return launch_grouped_direct<T, 64, 2, 2, 4, GATED>(a, st);
         }
     }
-    if (mean <= 8 || few <= 6 * kComputeUnits) return launch_grouped_rows<T, GATED>(a, st);
+    if (mean <= 8 || few <= 8 * kComputeUnits) return launch_grouped_rows<T, GATED>(a, st);
     if (mean >= 128 && rows / 128 * columns(128) >= 2 * kComputeUnits) return launch_grouped_tiles<T, 128, GATED>(a, st);
     return launch_grouped_tiles<T, 64, GATED>(a, st);
 }

@@ -370,7 +370,8 @@ __global__ void route_nothing_kernel(int32_t *starts, int32_t n)      // no toke
 
 static int chunk_tokens(int tokens)
 {
-    return tokens <= kOneChunk ? kOneChunk : (tokens + kChunks - 1) / kChunks > 16 ? (tokens + kChunks - 1) / kChunks : 16;
+    const int each = (tokens + kChunks - 1) / kChunks;
+    return each > kOneChunk ? each : kOneChunk;            // (as many as a workgroup takes at once)
 }
 
 static int check_route(const wpk_route_desc *dp)

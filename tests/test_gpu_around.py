@@ -555,8 +555,8 @@ GROUPED_FORMS = [("grouped_rows_kernel", (1, 2), "bf16", [1, 0, 3, 2], 200, 4200
                  ("grouped_direct_kernel", (256, 256, 2, 4, 64, 2), "bf16", [900, 300, 0, 1200], 8000, 328, False),
                  ("grouped_direct_kernel", (256, 256, 2, 4, 64, 2), "f16", [900, 300, 0, 1200], 4000, 200, True),
                  ("grouped_rows_kernel", (1, 2), "f32", [3, 9, 0, 20], 500, 1300, True), ("grouped_rows_kernel", (1, 2), "f32", [60, 33, 1], 700, 700, False),
-                 ("grouped_tiles_kernel", (64, 64, 2, 2), "f32", [90, 100, 0, 120], 2300, 140, False),
-                 ("grouped_tiles_kernel", (64, 64, 2, 2), "bf16", [90, 100, 0, 120], 1300, 141, True),
+                 ("grouped_tiles_kernel", (64, 64, 2, 2), "f32", [90, 100, 0, 120], 3000, 140, False),
+                 ("grouped_tiles_kernel", (64, 64, 2, 2), "bf16", [90, 100, 0, 120], 1500, 141, True),
                  ("grouped_tiles_kernel", (128, 128, 2, 2), "f32", [400, 300, 1, 500], 4000, 200, True),
                  ("grouped_tiles_kernel", (128, 128, 2, 2), "f16", [400, 300, 1, 500], 8000, 133, False),
                  ("linear_q8_rows_kernel", (1, 2), "e4m3", [1, 0, 17, 2], 300, 2900, True), ("linear_q8_rows_kernel", (1, 2), "e4m3", [5, 20, 0], 900, 5000, False),
