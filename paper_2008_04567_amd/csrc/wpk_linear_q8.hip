@@ -93,7 +93,8 @@ __global__ void __launch_bounds__(64 * WM * WN, (BM + BN) * 128 * STAGES > 73728
     __shared__ __align__(16) float scales[2][BM][8];
     static_assert(sizeof(lds) >= sizeof(float) * WM * WN * 32 * (16 * TN + 4), "what put_tile needs");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 15, g = lane >> 4;
-    const int wm = wave % WM, wn = wave / WM, slice = GROUPED ? 0 : blockIdx.y;
+    // (waves of different rows share a SIMD: where a tile has no rows for one of them, the other has it to itself)
+    const int wm = wave / WN, wn = wave % WN, slice = GROUPED ? 0 : blockIdx.y;
     TileAt at = {0, 0};
     if constexpr (GROUPED) {
         GroupTile tile;
@@ -205,12 +206,30 @@ __global__ void __launch_bounds__(64 * WM * WN, (BM + BN) * 128 * STAGES > 73728
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kUnderWay + kXLoads + 1) : "memory");
     __builtin_amdgcn_s_barrier();
     if (odd_k == k_begin) clear_tail(&lds[0][0], k_begin, 0);
+    int stage = 0, step = 0;
+    if (WM > 1 && m0 + wm * TM * 16 >= a.m) {                  // no rows for this wave: it loads, meets and clears as the others do
+        for (int k = k_begin; k < k_end; k += BK, ++step) {
+            const int next = stage == STAGES - 1 ? 0 : stage + 1;
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kUnderWay) : "memory");
+            __builtin_amdgcn_s_barrier();
+            if (k == odd_k) clear_tail(&lds[stage][0], k, 1);
+            fetch(stage, k + STAGES * BK, 0, kFirst);
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kUnderWay) : "memory");
+            __builtin_amdgcn_s_barrier();
+            if (k + BK == odd_k) clear_tail(&lds[next][0], k + BK, 0);
+            fetch_scales((step >> 3) + 1, step & (kScaleLoads - 1));
+            fetch(stage, k + STAGES * BK, kFirst, kLoads);
+            stage = next;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        return;
+    }
     i32x8 fw[TN], fx[2][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) fx[0][h] = read(&lds[0][0], x_at + 16 * h);
 #pragma unroll
     for (int j = 0; j < TN; ++j) fw[j] = read(&lds[0][0], w_at + 16 * j);
-    int stage = 0, step = 0;
     for (int k = k_begin; k < k_end; k += BK, ++step) {
         const int next = stage == STAGES - 1 ? 0 : stage + 1;
         uint8_t *const buf = &lds[stage][0], *const buf_next = &lds[next][0];
