@@ -537,7 +537,8 @@ int wpk_ssm_scan_step(const wpk_ssm_desc *d, const void *x, const void *dt, cons
  * What a served model puts around and between its sequence layers: the RMS norm with the residual's addition, matrix products
  * in 8 bits, and layers of experts (a router and products of rows sorted by expert).  The conventions are the sequence layers':
  * device pointers owned by the caller, rows dense within and `*_stride` elements apart, sums in 32 bits, values rounded once, when
- * stored, nothing allocated or kept, any call can be captured.  Tensors and stream belong to the current device.
+ * stored, nothing allocated or kept, any call can be captured.  Tensors and stream belong to the current device.  Products that
+ * would take 2^32 threads or more are refused (WPK_E_UNSUPPORTED).
  *
  * 8 bits.  A row of e4m3 values q has one fp32 scale for each 128 of them, rows of scales `*_scale_stride` elements apart: the row
  * stands for q[c] * scale[c / 128].  The last block may be shorter.  A weight has one scale for each block of 128 rows and 128

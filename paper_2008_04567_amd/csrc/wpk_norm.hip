@@ -3,6 +3,8 @@
 // Both are passes over memory (bound: its bytes; for few rows, a launch and two latencies).  A lane holds eight neighbouring
 // elements at a time, so a block of 128 values that share a scale is a row of 16 lanes, and its largest magnitude is found
 // without LDS.
+#include <type_traits>
+
 #include "wpk_q8.h"
 
 namespace wpk {
@@ -34,9 +36,11 @@ __device__ inline int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x +
 // result, so every input is read once; parts of a row are asked for four at a time.  16384 x 4096 bf16 with residual, into h and 8
 // bits: 87 us, 5.4 TB/s (a copy reaches 5.1); eight parts for each of 4096 rows of 2048: 32 us, 5.8 TB/s; 16 rows of 2048: 3.4 us,
 // of which a launch is most.
+// Rows beyond 32768 (P = 8) keep 40 to 140 registers in scratch memory.
 template <typename T, int LANES, int P, bool ALL, bool FAR> __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) rms_norm_kernel(NormArgs a)
 {
     const int kWaves = LANES / 64;
+    const bool kLong = P > 2;         // rows that take most registers: a part and a piece at a time, the gain when it is needed
     const int lane = threadIdx.x % LANES;
     const int64_t units = (int64_t)a.rows * a.groups;
     int64_t unit = workgroup();
@@ -47,7 +51,7 @@ template <typename T, int LANES, int P, bool ALL, bool FAR> __global__ void __la
     const int64_t row = a.groups == 1 ? unit : unit / a.groups;
     const int c0 = a.groups == 1 ? 0 : (int)(unit - row * a.groups) * a.width;
 
-    f32x8 s[P], gain[P];
+    f32x8 s[P];
     int left[P], at[P];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -69,53 +73,82 @@ template <typename T, int LANES, int P, bool ALL, bool FAR> __global__ void __la
             s[p] += v;
         }
     } else {
-        // four parts under way at a time; a row that is not there is read as one that is, and counts as zeros
-        for (int j0 = 0; j0 < a.parts; j0 += 4) {
-            f32x8 v[4][P];
-            float w[4];
+        // a row that is not there is read as one that is, and counts as zeros
+        auto add = [&](auto number, int j0) {
+            const int N = decltype(number)::value;             // parts under way at a time
+            f32x8 v[N][P];
+            float w[N];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t e = row * a.parts + min(j0 + j, a.parts - 1);
+            for (int j = 0; j < N; ++j) {
+                const int64_t e = row * a.parts + j0 + j;
                 const int64_t from = a.source ? a.source[e] : e;
-                const bool there = from >= 0 && from < a.x_rows && j0 + j < a.parts;
+                const bool there = from >= 0 && from < a.x_rows;
                 w[j] = there ? (a.weights ? a.weights[e] : 1.0f) : 0.0f;
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
+                    if constexpr (kLong) {
+                        const f32x8 u = Eight<T>::template load<ALL, FAR>(row_of(a.x, a.x_stride, there ? from : 0, p), left[p]);
+                        if (there) s[p] += u * w[j];
+                        __builtin_amdgcn_sched_barrier(0);
+                        continue;
+                    }
                     v[j][p] = Eight<T>::template load<ALL, FAR>(row_of(a.x, a.x_stride, there ? from : 0, p), left[p]);
                     if (!there) v[j][p] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
                 }
             }
+            if constexpr (kLong) return;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < N; ++j)
 #pragma unroll
                 for (int p = 0; p < P; ++p) s[p] += v[j][p] * w[j];
+        };
+        int j0 = 0;
+        if constexpr (!kLong) {
+            for (; j0 + 4 <= a.parts; j0 += 4) add(std::integral_constant<int, 4>(), j0);
+            if (a.parts - j0 >= 2) add(std::integral_constant<int, 2>(), j0), j0 += 2;
         }
+        for (; j0 < a.parts; ++j0) add(std::integral_constant<int, 1>(), j0);
     }
+    auto gain_of = [&](int p) {
+        return a.gain ? Eight<T>::template load<ALL, false>((const T *)a.gain + at[p], left[p]) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
+    };
+    f32x8 gain[kLong ? 1 : P];
+    if constexpr (!kLong)
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        if (a.gain) gain[p] = Eight<T>::template load<ALL, false>((const T *)a.gain + at[p], left[p]);
-        else gain[p] = f32x8{1, 1, 1, 1, 1, 1, 1, 1};
-    }
-    float sum = 0.0f;
+        for (int p = 0; p < P; ++p) gain[p] = gain_of(p);
+    __shared__ float part[2][kWaves];
+    auto squares = [&](float by, int turn) {                   // sum of (by s)^2 over the row
+        float sum = 0.0f;
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        const f32x8 e = s[p] * s[p];
-        sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+        for (int p = 0; p < P; ++p) {
+            const f32x8 u = s[p] * by, e = u * u;
+            sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+        }
+        sum = wave_sum(sum);
+        if (kWaves > 1) {
+            if ((lane & 63) == 0) part[turn][lane >> 6] = sum;
+            __syncthreads();
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) sum += part[turn][i];
+        }
+        return sum;
+    };
+#pragma unroll
+    for (int p = 0; p < P; ++p)
         if (a.h && (ALL || left[p] > 0)) Eight<T>::template store<ALL, FAR>((T *)a.h + row * a.h_stride + at[p], left[p], s[p]);
-    }
-    sum = wave_sum(sum);
-    if (kWaves > 1) {
-        __shared__ float part[kWaves];
-        if ((lane & 63) == 0) part[lane >> 6] = sum;
-        __syncthreads();
-        sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) sum += part[i];
-    }
-    const float r = rsqrtf(sum / (float)a.width + a.eps);
+    const float sum = squares(1.0f, 0);
+    float r = rsqrtf(sum / (float)a.width + a.eps);
+    // squares that are no 32-bit numbers, or no normal ones where eps does not hide them, are formed again of scaled values
+    const float by = sum > 3.4e38f ? 0x1p-80f : sum < 0x1p-90f && a.eps < 0x1p-90f ? 0x1p80f : 1.0f;
+    if (by != 1.0f) r = rsqrtf(squares(by, 1) / (float)a.width + a.eps * by * by) * by;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        const f32x8 v = s[p] * r * gain[p];
+        if constexpr (kLong) {
+            gain[0] = gain_of(p);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        const f32x8 v = s[p] * r * gain[kLong ? 0 : p];
         if (a.y && (ALL || left[p] > 0)) Eight<T>::template store<ALL, FAR>((T *)a.y + row * a.y_stride + at[p], left[p], v);
         // (a row's last block: the lanes behind it hold zeros)
         if (a.q) store_8<ALL, FAR>(a.q + row * a.q_stride + at[p], a.scales + row * a.scale_stride + at[p] / kScaleBlock, left[p], v, lane % 16 == 0);

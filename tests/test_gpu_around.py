@@ -82,10 +82,20 @@ def test_norm_infinities_and_nan_stay_in_their_rows(A):
         A.run_norm(4, width, "f32", edit=edit)
 
 
-@pytest.mark.parametrize("scale", [1e-18, 1e15])
+@pytest.mark.parametrize("scale", [1e-30, 1e-18, 1e15, 1e25, 1e37])
 def test_norm_small_and_large(A, scale):
     A.run_norm(3, 700, "f32", scale=scale, eps=0.0, q=True)
-    A.run_norm(3, 700, "bf16", scale=scale, eps=1e-6, q=True)
+    A.run_norm(3, 7000, "f32", scale=scale, eps=0.0)
+    A.run_norm(3, 700, "bf16", scale=scale, eps=1e-6)
+
+
+def test_norm_rows_of_zeros(A):
+    def zeros(x, res, g):
+        x[1], res[1] = 0.0, 0.0
+    for width in (64, 3000):
+        r = A.run_norm(3, width, "f32", edit=zeros, q=True)
+        assert not r["y"][1].any() and not A.numbers(r["q"])[1].any()
+        A.run_norm(3, width, "f32", edit=zeros, eps=0.0)       # nothing over nothing
 
 
 def test_norm_many_rows(A):
@@ -343,7 +353,7 @@ def test_route_sizes(A, dtype, n, k):
         A.run_route(A.Rng(tokens).normal((tokens, n), "f32", 2.0), k, dtype, normalize=tokens % 2 == 0, pad=tokens % 3)
 
 
-@pytest.mark.parametrize("tokens", [1, 63, 64, 65, 1000, 5000, 20000])
+@pytest.mark.parametrize("tokens", [1, 63, 64, 65, 1000, 5000, 20000, 200000])
 def test_route_tokens(A, tokens):
     A.run_route(A.Rng(tokens).normal((tokens, 60)), 6, "bf16", scale=2.5)
 
