@@ -120,12 +120,6 @@ template <typename T> __global__ void __launch_bounds__(256) linear_join_kernel(
 }
 
 // ---- rows by expert --------------------------------------------------------------------------------------------
-__device__ inline int lanes_total(int v)       // the sum over all lanes
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    return __builtin_amdgcn_readfirstlane(v);
-}
 __device__ inline int running_sum(int v)       // over the lanes up to this one
 {
     v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);       // row_shr 1, 2, 4, 8
@@ -167,37 +161,37 @@ struct GroupTile {
 template <int ROWS> __device__ inline bool take_group_tile(LinearArgs &a, int id, int tiles_n, size_t elem, size_t y_elem, GroupTile *out)
 {
     const int lane = threadIdx.x & 63;
-    int total = 0;
-    for (int g0 = 0; g0 < a.groups; g0 += 64) {
-        int first, length = 0;
+    int first = 0, length = 0, tiles = 0, upto = 0, total = 0;       // of the lane's expert; tiles up to it; tiles of all
+    auto look = [&](int g0, int before) {                            // at experts g0 .. g0 + 63
+        length = 0;
         if (g0 + lane < a.groups) group_rows(a, g0 + lane, &first, &length);
-        total += lanes_total((length + ROWS - 1) / ROWS);
-    }
+        tiles = (length + ROWS - 1) / ROWS;
+        upto = before + running_sum(tiles);
+        return __builtin_amdgcn_readlane(upto, 63);
+    };
+    for (int g = 0; g < a.groups; g += 64) total = look(g, total);
     const int all = total * tiles_n, each = all / kNumXcd, more = all % kNumXcd, die = id % kNumXcd;
     if (id / kNumXcd >= each + (die < more ? 1 : 0)) return false;
     const int t = die * each + min(die, more) + id / kNumXcd, want = t / tiles_n;
     out->n = t - want * tiles_n;
-    int before = 0;
-    for (int g0 = 0; g0 < a.groups; g0 += 64) {
-        int first = 0, length = 0;
-        if (g0 + lane < a.groups) group_rows(a, g0 + lane, &first, &length);
-        const int tiles = (length + ROWS - 1) / ROWS, upto = before + running_sum(tiles);
-        const uint64_t mine = __ballot(want >= upto - tiles && want < upto);
-        if (mine) {
-            const int of = __builtin_ctzll(mine);
-            const int skip = (want - __builtin_amdgcn_readlane(upto - tiles, of)) * ROWS;
-            const int r0 = __builtin_amdgcn_readlane(first, of) + skip;
-            out->group = g0 + of, out->row = r0;
-            a.m = min(ROWS, __builtin_amdgcn_readlane(length, of) - skip);
-            a.w = uniform((const char *)a.w + (g0 + of) * a.w_group_stride * (int64_t)elem);
-            a.y = uniform((char *)a.y + r0 * a.y_stride * (int64_t)y_elem);
-            if (a.source) a.source = uniform(a.source + r0);
-            else a.x = uniform((const char *)a.x + r0 * a.x_stride * (int64_t)elem);
-            return true;
+    int g0 = 0;
+    if (a.groups > 64)                                               // (up to 64 are looked at already)
+        for (int before = 0; g0 < a.groups; g0 += 64) {
+            const int end = look(g0, before);
+            if (want < end) break;
+            before = end;
         }
-        before = __builtin_amdgcn_readlane(upto, 63);
-    }
-    return false;
+    const uint64_t mine = __ballot(want >= upto - tiles && want < upto);
+    if (!mine) return false;
+    const int of = __builtin_ctzll(mine), skip = (want - __builtin_amdgcn_readlane(upto - tiles, of)) * ROWS;
+    const int r0 = __builtin_amdgcn_readlane(first, of) + skip;
+    out->group = g0 + of, out->row = r0;
+    a.m = min(ROWS, __builtin_amdgcn_readlane(length, of) - skip);
+    a.w = uniform((const char *)a.w + (g0 + of) * a.w_group_stride * (int64_t)elem);
+    a.y = uniform((char *)a.y + r0 * a.y_stride * (int64_t)y_elem);
+    if (a.source) a.source = uniform(a.source + r0);
+    else a.x = uniform((const char *)a.x + r0 * a.x_stride * (int64_t)elem);
+    return true;
 }
 
 // the row of x for row i of y (rows behind the last one count as it), and the row of w for row i of a tile of w

@@ -600,3 +600,106 @@ def test_norm_and_quantize_of_many_bytes(A):
     A.run_norm(2100, 1024, "bf16", parts=17, source="random", weights="random")
     eight(A, A.Rng(1).normal((8200, 2050)))
     eight(A, A.Rng(2).normal((270000, 130), "bf16"), pad=1, offset=1)
+
+
+# ---- offsets that pass 32 bits: the last rows, experts and values of tensors of more than 2^32 bytes ------------
+def test_norm_and_quantize_far_rows(A):
+    import torch
+    B, rows, width = A.B, 270000, 8192
+    x, last = torch.zeros((rows, width), device="cuda", dtype=torch.bfloat16), A.Rng(1).normal((3, width), "bf16")
+    x[-3:] = last
+    gain = A.Rng(2).normal((width,), "bf16")
+    out = []
+    for t in (x, last):
+        n = t.shape[0]
+        y, q, s = torch.empty_like(t), torch.empty((n, width), device="cuda", dtype=torch.uint8), torch.empty((n, 64), device="cuda")
+        B.rms_norm_fwd(B.make_rms_norm_desc(n, width), t, gain, y=y, q=q, scales=s)
+        out.append([v[-3:].clone() for v in (y, q, s)])
+        B.quantize_fwd(B.make_quantize_desc(n, width), t, q, s)
+        out[-1] += [v[-3:].clone() for v in (q, s)]
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+    # rows that are looked up
+    source, y = A.i32([[rows - 1, rows - 3], [0, rows - 2]]), torch.empty((2, width), device="cuda", dtype=torch.bfloat16)
+    B.rms_norm_fwd(B.make_rms_norm_desc(2, width, parts=2, x_rows=rows), x, None, h=y, source=source)
+    assert torch.equal(y[0], (last[2].float() + last[0].float()).bfloat16()) and torch.equal(y[1], last[1])
+
+
+def test_linear_q8_far_rows(A):
+    import torch
+    B, m, n, k = A.B, 270000, 72, 8192
+    small, xs, xv = A.in_8(A.Rng(1).normal((5, k)))
+    w, ws, wv = A.weight_in_8(A.Rng(2).normal((n, k), "f32", k ** -0.5))
+    x, scales = torch.zeros((m, k), device="cuda", dtype=torch.uint8), torch.ones((m, 64), device="cuda")
+    x[-5:], scales[-5:] = small, xs
+    y = torch.full((m, n), A.GUARD, device="cuda", dtype=torch.bfloat16)
+    desc = B.make_linear_q8_desc(m, n, k)
+    B.linear_q8_fwd(desc, x, scales, w, ws, y, workspace=A.workspace(B.linear_q8_workspace(desc)))
+    ref, d = A.osq.linear(xv, wv)
+    A.close(y[-5:], ref, d, "bf16", (k + 64) * 2.0 ** -24 + 7 * 2.0 ** -13, "the last rows")
+    assert not y[:-5].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("rows", [3, 150])
+def test_grouped_far_experts_and_rows(A, dtype, rows):
+    import torch
+    B, E, n, k = A.B, 40 if dtype == "bf16" else 70, 4096, 8192
+    far_rows = 270000 if dtype == "bf16" else 40000        # 8-bit rows that are looked up end at 2^31 bytes
+    ty = torch.bfloat16 if dtype == "bf16" else torch.uint8
+    w, x = torch.zeros((E, 2 * n, k), device="cuda", dtype=ty), torch.zeros((far_rows, k), device="cuda", dtype=ty)
+    r, kw = A.Rng(rows), {}
+    if dtype == "bf16":
+        last, lw = r.normal((rows, k), dtype), r.normal((48, k), dtype, k ** -0.5)
+        xv, wv = A.f64(last), A.f64(lw)
+    else:
+        last, xs, xv = A.in_8(r.normal((rows, k)))
+        parts = [A.weight_in_8(r.normal((24, k), "f32", k ** -0.5)) for _ in range(2)]
+        lw, wv = torch.cat([p[0] for p in parts]), np.concatenate([p[2] for p in parts])
+        x_scales, w_scales = torch.ones((far_rows, 64), device="cuda"), torch.ones((E, 2, 32, 64), device="cuda")
+        x_scales[-rows:], w_scales[-1, :, -1:] = xs, torch.stack([p[1] for p in parts])   # the last columns' block
+        kw = dict(x_scales=x_scales, w_scales=w_scales)
+    x[-rows:], w[-1, n - 24:n], w[-1, 2 * n - 24:] = last, lw[:24], lw[24:]
+    y = torch.empty((rows, n), device="cuda", dtype=torch.bfloat16)
+    desc = B.make_grouped_linear_desc(E, rows, n, k, dtype=B.BF16 if dtype == "bf16" else B.E4M3, act=B.ACT_SILU, gated=True, x_rows=far_rows)
+    source = A.i32(list(range(far_rows - rows, far_rows)))
+    B.grouped_linear_fwd(desc, x, w, A.i32([0] * E + [rows]), y, source=source, **kw)
+    ref, d = A.oa.grouped(xv, wv[None], [0, rows], None, "silu", True)
+    share = (k + 64) * 2.0 ** -24 + 2.0 ** -19 + (7 * 2.0 ** -13 if dtype == "e4m3" else 0.0)
+    A.close(y[:, -24:], ref, d, "bf16", share, "the last expert's last columns")
+    assert not y[:, :-24].any()
+    if dtype == "e4m3":
+        many = B.make_grouped_linear_desc(E, rows, n, k, dtype=B.E4M3, gated=True, x_rows=1 << 18)
+        with pytest.raises(B.WpkError) as e:
+            B.grouped_linear_fwd(many, x, w, A.i32([0] * E + [rows]), y, source=source, **kw)
+        assert e.value.status == B.E_UNSUPPORTED
+
+
+def test_two_graphs_that_share_a_workspace(A):
+    import torch
+    B, calls = A.B, []
+    room = None
+    for seed, (m, n, k) in enumerate(((3, 300, 5000), (130, 1030, 4096))):
+        x, xs, _ = A.in_8(A.Rng(seed).normal((m, k)))
+        w, ws, _ = A.weight_in_8(A.Rng(seed + 9).normal((n, k)))
+        desc, y = B.make_linear_q8_desc(m, n, k), torch.empty((m, n), device="cuda", dtype=torch.bfloat16)
+        assert B.linear_q8_workspace(desc) > 0
+        calls.append((desc, x.contiguous() if x.stride(0) == desc.x_stride else x, xs, w, ws, y))
+        calls[-1][0].x_stride, calls[-1][0].w_stride = x.stride(0), w.stride(0)
+    room = A.workspace(max(B.linear_q8_workspace(c[0]) for c in calls))
+    run = lambda c: B.linear_q8_fwd(*c, workspace=room, stream=torch.cuda.current_stream())
+    graphs, want = [], []
+    for c in calls:
+        run(c)
+        torch.cuda.synchronize()
+        want.append(c[5].clone())
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            run(c)
+    for turn in range(3):
+        for c in calls:
+            c[5].zero_()
+        for g in graphs if turn % 2 else graphs[::-1]:
+            g.replay()
+        run(calls[turn % 2])
+        torch.cuda.synchronize()
+        assert all(torch.equal(c[5], t) for c, t in zip(calls, want)), "replay %d" % turn
