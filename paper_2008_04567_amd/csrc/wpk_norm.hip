@@ -21,13 +21,6 @@ struct NormArgs {
     int64_t x_stride, residual_stride, h_stride, y_stride, q_stride, scale_stride;
 };
 
-__device__ inline float wave_sum(float v)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    return v;
-}
-
 // the number of this workgroup, in a grid of two dimensions
 __device__ inline int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
@@ -124,7 +117,7 @@ template <typename T, int LANES, int P, bool ALL, bool FAR> __global__ void __la
             const f32x8 u = s[p] * by, e = u * u;
             sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
         }
-        sum = wave_sum(sum);
+        sum = wave_total(sum);
         if (kWaves > 1) {
             if ((lane & 63) == 0) part[turn][lane >> 6] = sum;
             __syncthreads();

@@ -120,17 +120,6 @@ template <typename T> __global__ void __launch_bounds__(256) linear_join_kernel(
 }
 
 // ---- rows by expert --------------------------------------------------------------------------------------------
-__device__ inline int running_sum(int v)       // over the lanes up to this one
-{
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);       // row_shr 1, 2, 4, 8
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);       // lane 15 of a row to the next row
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);       // lane 31 to the next two rows
-    return v;
-}
-
 // first row and rows of expert g
 __device__ inline void group_rows(const LinearArgs &a, int g, int *first, int *length)
 {
@@ -166,7 +155,7 @@ template <int ROWS> __device__ inline bool take_group_tile(LinearArgs &a, int id
         length = 0;
         if (g0 + lane < a.groups) group_rows(a, g0 + lane, &first, &length);
         tiles = (length + ROWS - 1) / ROWS;
-        upto = before + running_sum(tiles);
+        upto = before + running_sum_32(tiles);
         return __builtin_amdgcn_readlane(upto, 63);
     };
     for (int g = 0; g < a.groups; g += 64) total = look(g, total);

@@ -71,21 +71,6 @@ __device__ inline uint32_t wave_max(uint32_t v)
     v = max_of_lane_before<0x143, 0xc>(v);
     return __builtin_amdgcn_readlane((int)v, 63);
 }
-template <int CTRL, int ROWS> __device__ inline float add_of_lane_before(float v)
-{
-    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, true));
-}
-__device__ inline float wave_total(float v)
-{
-    v = add_of_lane_before<0x111, 0xf>(v);
-    v = add_of_lane_before<0x112, 0xf>(v);
-    v = add_of_lane_before<0x114, 0xf>(v);
-    v = add_of_lane_before<0x118, 0xf>(v);
-    v = add_of_lane_before<0x142, 0xa>(v);
-    v = add_of_lane_before<0x143, 0xc>(v);
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
-}
-
 // What follows the choice, in the lanes that have one: `key` is its, `top` the largest, `all` the sum of exp(logit - top) over all
 // experts or, normalized, over the chosen.
 __device__ inline void put_choice(const RouteArgs &a, int64_t at, int expert, float weight, float top, float all)
@@ -208,12 +193,7 @@ template <typename T, int PER> __device__ inline int choose_by_row(const RouteAr
 __device__ inline int sum_before(int v, int *room)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int upto = v;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
-    }
+    const int upto = running_sum_32(v);
     if (lane == 63) room[wave] = upto;
     __syncthreads();
     int before = upto - v;

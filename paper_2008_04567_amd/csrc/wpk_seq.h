@@ -77,6 +77,27 @@ __device__ inline double running_sum(double v)
     return v;
 }
 
+// ... and in 32 bits
+template <int CTRL, int ROWS> __device__ inline int lanes_before(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, true); }
+template <int CTRL, int ROWS> __device__ inline float lanes_before(float v)
+{
+    return __builtin_bit_cast(float, lanes_before<CTRL, ROWS>(__builtin_bit_cast(int, v)));
+}
+template <typename V> __device__ inline V running_sum_32(V v)
+{
+    v += lanes_before<0x111, 0xf>(v);
+    v += lanes_before<0x112, 0xf>(v);
+    v += lanes_before<0x114, 0xf>(v);
+    v += lanes_before<0x118, 0xf>(v);
+    v += lanes_before<0x142, 0xa>(v);
+    v += lanes_before<0x143, 0xc>(v);
+    return v;
+}
+__device__ inline float wave_total(float v)            // over all lanes, in all of them
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, running_sum_32(v)), 63));
+}
+
 __device__ inline double read_lane(double v, int lane)
 {
     const uint64_t b = __builtin_bit_cast(uint64_t, v);
