@@ -442,7 +442,9 @@ template <typename T, int BM, int BN, int WM, int WN, bool GROUPED, bool GATED> 
     part_t *const lds = (part_t *)shared;              // [part][rows of w, then rows of x][kRow]
     const int kPart = (BM + BN) * kRow;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 31, half = lane >> 5;
-    const int wm = wave % WM, wn = wave / WM, slice = GROUPED ? 0 : blockIdx.y, kOut = GATED ? BN / 2 : BN;
+    // (by expert, waves of different rows share a SIMD: where a tile has no rows for one of them, the other has it to itself)
+    const int wm = GROUPED ? wave / WN : wave % WM, wn = GROUPED ? wave % WN : wave / WM, slice = GROUPED ? 0 : blockIdx.y;
+    const int kOut = GATED ? BN / 2 : BN;
     TileAt at = {0, 0};
     if constexpr (GROUPED) {
         GroupTile tile;
@@ -452,6 +454,7 @@ template <typename T, int BM, int BN, int WM, int WN, bool GROUPED, bool GATED> 
         at = tile_of(blockIdx.x, (a.m + BM - 1) / BM, (a.n + BN - 1) / BN);
     }
     const int m0 = at.m * BM, n0 = at.n * kOut;
+    const bool idle = GROUPED && m0 + wm * TM * 32 >= a.m;     // no rows of the tile are this wave's: it loads and meets alone
     const int k_begin = slice * a.slice_k, k_end = min(a.k, k_begin + a.slice_k);
 
     const T *src[kPer];
@@ -519,7 +522,7 @@ template <typename T, int BM, int BN, int WM, int WN, bool GROUPED, bool GATED> 
             const int next = min(k + BK, k_whole - BK);
 #pragma unroll
             for (int i = 0; i < kPer; ++i) held[i] = Octet<T>::load(src[i] + next);
-            multiply();
+            if (!idle) multiply();
             __syncthreads();
         }
     }
@@ -529,9 +532,10 @@ template <typename T, int BM, int BN, int WM, int WN, bool GROUPED, bool GATED> 
             held[i] = Octet<T>::load_some(src[i] + k_whole, k_end - k_whole - (tid + i * kThreads) % kOctets * 8);
         stage();
         __syncthreads();
-        multiply();
+        if (!idle) multiply();
         __syncthreads();
     }
+    if (idle) return;
 
     float scale = 1.0f;
     bool odd = false;                 // infinities, NaN, or numbers that the scaled parts could not hold
@@ -576,7 +580,9 @@ __device__ __forceinline__ void product_direct(LinearArgs &a)
     __shared__ __align__(16) T lds[STAGES][(BM + BN) * BK];    // rows of w, then rows of x
     static_assert(sizeof(lds) >= sizeof(float) * WM * WN * 32 * (32 * TN + 4), "what put_tile needs");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 31, half = lane >> 5;
-    const int wm = wave % WM, wn = wave / WM, slice = GROUPED ? 0 : blockIdx.y, kOut = GATED ? BN / 2 : BN;
+    // (by expert, waves of different rows share a SIMD: where a tile has no rows for one of them, the other has it to itself)
+    const int wm = GROUPED ? wave / WN : wave % WM, wn = GROUPED ? wave % WN : wave / WM, slice = GROUPED ? 0 : blockIdx.y;
+    const int kOut = GATED ? BN / 2 : BN;
     TileAt at = {0, 0};
     if constexpr (GROUPED) {
         GroupTile tile;
@@ -586,6 +592,7 @@ __device__ __forceinline__ void product_direct(LinearArgs &a)
         at = tile_of(blockIdx.x, (a.m + BM - 1) / BM, (a.n + BN - 1) / BN);
     }
     const int m0 = at.m * BM, n0 = at.n * kOut;
+    const bool idle = GROUPED && m0 + wm * TM * 32 >= a.m;     // no rows of the tile are this wave's: it loads and meets alone
     const int k_begin = slice * a.slice_k, k_end = min(a.k, k_begin + a.slice_k);
     auto order = [](int r) { return BK == 64 ? (r >> 1) & 7 : (r >> 2) & 3; };
 
@@ -655,8 +662,22 @@ __device__ __forceinline__ void product_direct(LinearArgs &a)
     for (int s = 0; s < STAGES; ++s) fetch(s, k_begin + s * BK, 0, s + 1 < STAGES ? kLoads : kShare);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * kLoads + kShare) : "memory");
     __builtin_amdgcn_s_barrier();
-    read_block(0, 0);
     int stage = 0;
+    if constexpr (GROUPED) {
+        if (idle) {
+            for (int k = k_begin; k < k_end; k += BK) {
+                fetch(stage == 0 ? STAGES - 1 : stage - 1, k + (STAGES - 1) * BK, kShare, kLoads);
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * kLoads) : "memory");
+                __builtin_amdgcn_s_barrier();
+                fetch(stage, k + STAGES * BK, 0, kShare);
+                stage = stage == STAGES - 1 ? 0 : stage + 1;
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            return;
+        }
+    }
+    read_block(0, 0);
     for (int k = k_begin; k < k_end; k += BK) {
         const int next = stage == STAGES - 1 ? 0 : stage + 1;
 #pragma unroll
