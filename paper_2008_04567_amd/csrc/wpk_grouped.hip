@@ -35,18 +35,19 @@ template <typename T, int B, bool GATED> static int launch_grouped_tiles(const L
 // By the mean of the experts' rows and the workgroups there would be.  us, experts x columns x reduction (gated: twice the columns),
 // rows of uneven spread:
 //   bf16, rows kernel / tiles of 64 / 128 (two steps in LDS) / 256
-//     8 x 2048 x 2048           mean 1: 13 / 14 / 26 / 49      64: 61 / 24 / 36 / 59     256: - / 54 / 48 / 66    1024: - / 173 / 116 / 121
-//     64 x 1024 x 2048, gated   mean 4: 99 / 106 / 123 / 140   64: 453 / 148 / 152 / 192  128: 850 / 215 / 162 / 202   256: - / 359 / 242 / 216
-//     64 x 2048 x 1536          mean 4: 86 / 77               64 x 2048 x 1024           mean 4: 62 / 57
-//     16 x 4096 x 4096          mean 1: 60 / 77               4: 92 / 101
-//     7 x 300 x 520             mean 95: 6.0 / 7.1 / 10
+//     8 x 2048 x 2048           mean 1: 13 / 13 / 24 / 39      64: 58 / 23 / 36 / 55     256: - / 55 / 47 / 64    1024: - / 176 / 117 / 120
+//     64 x 1024 x 2048, gated   mean 4: 95 / 105 / 121 / 134   64: 439 / 144 / 154 / 184  128: 826 / 209 / 169 / 193   256: - / 354 / 241 / 213
+//     64 x 2048 x 1536          mean 4: 82 / 75               64 x 2048 x 1024           mean 4: 58 / 55
+//     16 x 4096 x 4096          mean 1: 59 / 76               4: 90 / 100
+//     7 x 300 x 520             mean 95: 6.5 / 6.9 / 10
 //   (128 with four steps in LDS, for workgroups that have a compute unit to themselves: 8 x 2048 x 2048, mean 128, 26 against 37)
 //   fp32, rows kernel / tiles of 64 / 128
-//     8 x 2048 x 2048           mean 1: 28 / 89 / 157          32: 80 / 92 / 162         64: 119 / 94 / 162
-//     64 x 1024 x 2048, gated   mean 8: 222 / 294 / 402        16: 304 / 310 / 403      128: 1669 / 679 / 621
-//     128 x 768 x 1024, gated   mean 8: 205 / 223 / 313        16: 281 / 229 / 321
-//     16 x 2008 x 1024          mean 13: 47 / 54              20: 57 / 55               30: 76 / 55
-//     7 x 300 x 520             mean 95: 10 / 24 / 48
+//     8 x 2048 x 2048           mean 1: 28 / 74 / 115          32: 77 / 77 / 118         64: 116 / 79 / 119
+//     64 x 1024 x 2048, gated   mean 8: 215 / 232 / 301        16: 295 / 256 / 299       128: 1630 / 654 / 530
+//     128 x 768 x 1024, gated   mean 4: 169 / 168 / 228        8: 202 / 180 / 234        16: 274 / 193 / 235
+//     16 x 2008 x 1024          mean 13: 46 / 47              20: 55 / 48               30: 73 / 49
+//     32 x 512 x 512            mean 16: 16 / 18 / 37         64: 33 / 23 / 39
+//     7 x 300 x 520             mean 95: 10 / 19 / 41
 template <typename T, bool GATED> static int grouped_typed(const LinearArgs &a, bool direct, hipStream_t st)
 {
     const int64_t rows = a.m, groups = a.groups, mean = rows / groups, out = GATED ? 16 : 32;

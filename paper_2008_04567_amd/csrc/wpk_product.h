@@ -130,12 +130,6 @@ __device__ inline void group_rows(const LinearArgs &a, int g, int *first, int *l
     }
 }
 
-// Leaves of `a` the problem of one tile: up to ROWS rows of one expert, its weights, and which of tiles_n tiles of columns; false
-// where `id` is behind the last tile.  The number of tiles is known on the device alone: the grid has as many workgroups as there
-// could be, and those that have work are dealt out to the dies in equal runs, in which an expert's tiles of columns are next to
-// each other.  Every wave finds its tile by itself: two loads a lane for each 64 experts, and sums over lanes.  256
-// rows through 64 gated experts of 1024 x 2048 in bf16, by the row kernel: 99 us, 5.3 TB/s of weights; 65536 rows, by tiles of 256: 599
-// us, 0.92 PFLOP/s, an eighth of it rows that experts' last tiles do not have.
 // an address that all lanes have, where the compiler can see it
 template <typename P> __device__ inline P *uniform(P *p)
 {
@@ -144,6 +138,12 @@ template <typename P> __device__ inline P *uniform(P *p)
     return (P *)((uint64_t)hi << 32 | lo);
 }
 
+// Leaves of `a` the problem of one tile: up to ROWS rows of one expert, its weights, and which of tiles_n tiles of columns; false
+// where `id` is behind the last tile.  The number of tiles is known on the device alone: the grid has as many workgroups as there
+// could be, and those that have work are dealt out to the dies in equal runs, in which an expert's tiles of columns are next to
+// each other.  Every wave finds its tile by itself: two loads a lane for each 64 experts, and sums over lanes.  256
+// rows through 64 gated experts of 1024 x 2048 in bf16, by the row kernel: 95 us, 5.6 TB/s of weights; 65536 rows, by tiles of 256: 595
+// us, 0.92 PFLOP/s, an eighth of it rows that experts' last tiles do not have.
 struct GroupTile {
     int n, group, row;                // which tile of columns, the expert, the tile's first row of y
 };

@@ -259,7 +259,7 @@ __device__ inline void place_runs(const RouteArgs &a, const Runs &r, const int32
 }
 
 // A workgroup chooses for a chunk of tokens, and counts its experts; the only chunk is put in order as well.  32 tokens of 64 experts,
-// eight chosen, fp32: 5.5 us, all of it; 16384 tokens of 128, bf16: 6.9 us and 7.0 for the order (a wave a token took 12.4).
+// eight chosen, fp32: 5.3 us, all of it; 16384 tokens of 128, bf16: 7.1 us and 6.7 for the order (a wave a token took 12.4).
 template <typename T, int PER, bool ROW> __global__ void __launch_bounds__(kRouteThreads) route_choose_kernel(RouteArgs a)
 {
     __shared__ int counts[8 * kMostExperts], room[kRouteWaves], ids[kOneChunk * kMostChosen];
