@@ -50,6 +50,8 @@ class Experts:
             raise ValueError("h: values of a row stand one after another, rows apart")
         if not h.is_cuda:
             raise ValueError("the layer is not on the GPU")
+        if h.device.index != torch.cuda.current_device():      # (launches go to the current one)
+            raise ValueError("the layer is on %s, the current device is %d" % (h.device, torch.cuda.current_device()))
         return plan.run(h, stream)
 
 

@@ -51,6 +51,29 @@ def test_layer_is_its_formula(A, dtype, eight, tokens):
     assert err <= 3 * u + (2.0 ** -4 if eight else 0.0) + 2.0 ** -18, err
 
 
+@pytest.mark.parametrize("eight", [False, True])
+def test_no_tokens(A, eight):
+    """A batch that happens to be empty: no rows of any expert, and the next call is none the worse."""
+    import torch
+    from paper_2008_04567_amd.experts import Experts
+    m = Experts(96, 64, 6, 2, eight=eight, seed=1)
+    h = A.Rng(1).normal((3, 96), "bf16")
+    p, none = m.plan(3), m.plan(0)
+    first = m.run(p, h).clone()
+    assert tuple(m.run(none, h[:0]).shape) == (0, 96) and none.starts.tolist() == [0] * 7
+    assert torch.equal(first, m.run(p, h))
+
+
+def test_another_current_device_is_refused(A, monkeypatch):
+    import torch
+    from paper_2008_04567_amd.experts import Experts
+    m = Experts(96, 64, 6, 2, seed=1)
+    p, h = m.plan(3), A.Rng(1).normal((3, 96), "bf16")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: h.device.index + 1)
+    with pytest.raises(ValueError, match="current device"):
+        m.run(p, h)
+
+
 def test_rows_may_be_slices_and_calls_repeat(A):
     import torch
     from paper_2008_04567_amd.experts import Experts
