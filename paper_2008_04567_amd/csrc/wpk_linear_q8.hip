@@ -80,12 +80,13 @@ typedef const __attribute__((address_space(4))) float *Constants;     // read by
 // eight rows' for eight steps, the next eight steps' again and again until these begin, so that the same number of loads is always
 // under way.  (Every other eight rows have the two halves of the eight steps exchanged, so that 16 rows' scales of a step take 16
 // banks.)
-// 16384 x 4096 x 4096, bf16: 255 us, 285 with a residual, 1.93 PFLOP/s (a library product with one scale for all takes 192 and no
-// residual).  A step of 256 x 256 takes 1.7 us on a full device where its products alone take 1.04 (the matrix pipes are busy 44 % of
-// the cycles), 1.3 on one workgroup alone.  Without its loads it takes 1.4, without the multiplications by scales 1.4, and fewer
-// cycles came with lower clocks (2.28 to 2.12 GHz): what is left is bound by power more than by any unit.  52 us of the whole, 73
-// with a residual, are beginnings and ends of tiles (from times at reductions of 128 and more), where all compute units write at once.  Tried without gain: one meeting a step, four steps in LDS (one workgroup a
-// compute unit instead of three: 24 against 13.5 us for 65 x 8512 x 2048), waves of 64 x 64 in tiles of 128, tiles of 128 x 256.
+// 16384 x 4096 x 4096, bf16: 255 us, 274 to 285 with a residual, 1.93 PFLOP/s and more (a library product with one scale for all
+// takes 192 and no residual).  A step of 256 x 256 takes 1.7 us on a full device where its products alone take 1.04 (the matrix pipes are
+// busy 44 % of the cycles), 1.3 on one workgroup alone.  Without its loads it takes 1.4, without the multiplications by scales 1.4,
+// and fewer cycles came with lower clocks (2.28 to 2.12 GHz): what is left is bound by power more than by any unit.  52 us of the
+// whole, 73 with a residual, are beginnings and ends of tiles (from times at reductions of 128 and more), where all compute units
+// write at once.  Tried without gain: one meeting a step, four steps in LDS (one workgroup a compute unit instead of three: 24 against
+// 13.5 us for 65 x 8512 x 2048), waves of 64 x 64 in tiles of 128, tiles of 128 x 256, a tile's residual asked for a block ahead.
 template <typename T, int BM, int BN, int WM, int WN, int STAGES, bool GROUPED, bool GATED>
 __global__ void __launch_bounds__(64 * WM * WN, (BM + BN) * 128 * STAGES > 73728 ? WM * WN / 4 : WM * WN / 2) linear_q8_kernel(Q8Args q)
 {
