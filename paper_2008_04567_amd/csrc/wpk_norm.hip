@@ -132,9 +132,17 @@ template <typename T, int LANES, int P, bool ALL, bool FAR> __global__ void __la
         if (a.h && (ALL || left[p] > 0)) Eight<T>::template store<ALL, FAR>((T *)a.h + row * a.h_stride + at[p], left[p], s[p]);
     const float sum = squares(1.0f, 0);
     float r = rsqrtf(sum / (float)a.width + a.eps);
-    // squares that are no 32-bit numbers, or no normal ones where eps does not hide them, are formed again of scaled values
-    const float by = sum > 3.4e38f ? 0x1p-80f : sum < 0x1p-90f && a.eps < 0x1p-90f ? 0x1p80f : 1.0f;
-    if (by != 1.0f) r = rsqrtf(squares(by, 1) / (float)a.width + a.eps * by * by) * by;
+    // Squares that are no 32-bit numbers, or no normal ones where eps does not hide them, are formed again of scaled values.  The
+    // scale and the root stay two factors, since the reciprocal root of the whole may be no 32-bit number itself (above 2^128 for
+    // rows of the smallest numbers, below 2^-126 for those of the largest), in the order in which no product leaves the range:
+    // values grow before they meet the root, or meet it before they shrink.
+    const float by = sum > 3.4e38f ? 0x1p-80f : sum < 0x1p-90f && a.eps < 0x1p-90f ? 0x1p100f : 1.0f;
+    if (by != 1.0f) {
+        const float root = rsqrtf(squares(by, 1) / (float)a.width + a.eps * by * by), first = by > 1.0f ? by : root;
+        r = by > 1.0f ? root : by;
+#pragma unroll
+        for (int p = 0; p < P; ++p) s[p] *= first;
+    }
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         if constexpr (kLong) {
