@@ -547,8 +547,11 @@ int wpk_ssm_scan_step(const wpk_ssm_desc *d, const void *x, const void *dt, cons
  * From a row v in 32 bits they are made so: scale = max |v| of the block / 448, at least 2^-110, inverse = 1 / scale, q = v * inverse
  * rounded to the nearest e4m3 number, ties to even, none beyond 448.  A NaN stays one and leaves the rest of its block alone; a
  * block with an infinity has an infinite scale, and no value of it means a number.
- * Products of 8-bit values into a y of 16 bits add eight neighbouring entries' products with 13 bits below the largest of them (a
- * sum is off by some 2e-5 of itself; y's own rounding is 2^-9 or 2^-12); into a y of 32 bits they are added in 32 bits.
+ * Products of 8-bit values into a y of 16 bits: those of entries 8 i .. 8 i + 7 are added with 13 bits below the largest of the eight,
+ * so each of the other seven may lose up to 2^-13 of it, and a sum is off by at most 7 2^-13 (8.5e-4) of what its eights' largest
+ * magnitudes add up to.  Entries of one size lose far less, 1.6e-5 of a sum of normal ones.  Where single entries are far larger than
+ * their neighbours the loss may pass a f16 y's own rounding (2^-12 to 2^-11), and where large terms cancel any y's: a y of 32 bits has
+ * its products added in 32 bits, at some half the speed of large products.
  */
 
 /* For every row t, with `parts` rows of x to it:

@@ -23,9 +23,13 @@ __device__ inline bf16x8 widen(int32_t lo, int32_t hi)
 // The product of 16 x 16 by 128 entries: lane l holds 32 entries of row l % 16 of either operand.  (Which 32 does not matter as
 // long as both operands have them alike.)
 // The matrix instruction for 8 bits adds the products of eight neighbouring entries of a lane with 13 bits below the largest of
-// them (measured: beside 2^16, 2^3 is kept and 2^2 is not; of different eights everything is), so a sum is off by 1.6e-5 of
-// itself where entries are normal: a twentieth of an f16 y's own rounding.  For a y of 32 bits the operands are widened to bf16,
-// whose products are added in 32 bits, at half the rate.
+// them (measured: beside 2^16, 2^3 is kept and 2^2 is not, also where a -2^16 takes the 2^16 away; of different eights everything that
+// 32 bits hold is; the instruction for 32 entries does the same).  Seven of an eight lose up to 2^-13 of the largest each: a sum is off
+// by 7 2^-13 of the eights' largest magnitudes at most, by 1.6e-5 of itself where entries are normal, by some 1e-4 where every
+// eight has one product of 2^15 beside such of 2^1, and by half where two of 2^15 cancel in every eight.  Values of 8 bits are off by up
+// to 2^-4 themselves, so a y of 16 bits takes that for twice the rate.  For a y of 32 bits the operands are widened to bf16, whose
+// products are added in 32 bits: 16384 x 4096 x 4096 578 us against 247, 2048 x 4096 x 4096 82 against 54, 32 x 8512 x 2048 7.7 either
+// way.  (In tiles of 256 and 128 the widened operands would not fit the registers.)
 struct Operand8 {
     i32x8 v;
     __device__ static Operand8 of(i32x8 v) { return {v}; }
