@@ -60,6 +60,12 @@ def check_8(q, scales, v, tol, what):
     assert (err <= allowed).all(), "%s: 8-bit values, worst %.3g times the tolerance" % (what, (err / allowed).max())
 
 
+def after_inputs(stream):
+    """Inputs, workspaces and what outputs hold before a call are made on the current stream: a call on another waits for them."""
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+
+
 def run_norm(rows, width, dtype, groups=1, parts=1, residual=True, gain=True, y=True, q=False, h=True, source=None, weights=None,
              x_rows=None, pad=0, offset=0, eps=1e-5, seed=1, scale=1.0, edit=None, in_place=None, stream=None):
     r = Rng(seed)
@@ -86,8 +92,9 @@ def run_norm(rows, width, dtype, groups=1, parts=1, residual=True, gain=True, y=
     desc = B.make_rms_norm_desc(rows, width, groups=groups, parts=parts, x_rows=x_rows, dtype=code, eps=eps, x_stride=width + pad,
                                 residual_stride=width + pad, h_stride=width + pad, y_stride=width + pad,
                                 q_stride=-(-width // 16) * 16 + 32, scale_stride=nb + 1)
-    B.rms_norm_fwd(desc, x, g, y=yo, q=qo, scales=so, residual=res, h=ho, source=None if source is None else i32(source),
-                   weights=None if weights is None else torch.from_numpy(weights).cuda(), stream=stream)
+    on_device = dict(source=None if source is None else i32(source), weights=None if weights is None else torch.from_numpy(weights).cuda())
+    after_inputs(stream)
+    B.rms_norm_fwd(desc, x, g, y=yo, q=qo, scales=so, residual=res, h=ho, stream=stream, **on_device)
     torch.cuda.synchronize()
     s, d, v = oa.rms_norm(before[0], f64(g), eps, before[1], groups, parts, source, weights)
     e = (parts + 2) * 2.0 ** -24
@@ -153,7 +160,9 @@ def run_linear_q8(m, n, k, dtype, act="none", bias=True, residual=True, extra=0,
         y, yb = res, None
     desc = B.make_linear_q8_desc(m, n, k, dtype=code, act=ACTS[act], x_stride=x.stride(0), w_stride=w.stride(0), y_stride=n + pad,
                                  residual_stride=n + pad)
-    B.linear_q8_fwd(desc, x, xs, w, ws, y, bias=bb, residual=res, workspace=workspace(B.linear_q8_workspace(desc)), stream=stream)
+    room = workspace(B.linear_q8_workspace(desc))
+    after_inputs(stream)
+    B.linear_q8_fwd(desc, x, xs, w, ws, y, bias=bb, residual=res, workspace=room, stream=stream)
     torch.cuda.synchronize()
     if yb is not None:
         guard_intact(y, yb)
@@ -201,9 +210,10 @@ def run_grouped(lengths, n, k, dtype, y_dtype=None, act="none", gated=False, gat
     y, yb = out_rows(rows, n, n + pad, offset, TYPES[y_dtype][1])
     desc = B.make_grouped_linear_desc(groups, rows, n, k, dtype=code, y_dtype=TYPES[y_dtype][0], act=ACTS[act], gated=gated,
                                       x_rows=x_rows, y_stride=n + pad, **strides)
-    B.grouped_linear_fwd(desc, x, w, i32(st if starts is None else starts) if groups > 1 or before or behind else None, y,
-                         source=None if source is None else i32(source),
-                         workspace=workspace(B.grouped_linear_workspace(desc)), stream=stream, **kw)
+    first = i32(st if starts is None else starts) if groups > 1 or before or behind else None
+    kw.update(source=None if source is None else i32(source), workspace=workspace(B.grouped_linear_workspace(desc)))
+    after_inputs(stream)
+    B.grouped_linear_fwd(desc, x, w, first, y, stream=stream, **kw)
     torch.cuda.synchronize()
     guard_intact(y, yb)
     mine = slice(before, before + sum(lengths))
@@ -226,8 +236,9 @@ def run_route(logits, k, dtype, normalize=True, scale=1.0, order=True, pad=0, st
     starts, source = torch.full((n + 2,), -7, dtype=torch.int32, **dev), torch.full((tokens * k + 1,), -7, dtype=torch.int32, **dev)
     place = torch.full((tokens, k), -7, dtype=torch.int32, **dev)
     desc = B.make_route_desc(tokens, n, k, dtype=code, normalize=normalize, scale=scale, logits_stride=n + pad)
-    B.route_fwd(desc, l, experts, weights, *((starts, source, place) if order else ()),
-                workspace=workspace(B.route_workspace(desc)), stream=stream)
+    room = workspace(B.route_workspace(desc))
+    after_inputs(stream)
+    B.route_fwd(desc, l, experts, weights, *((starts, source, place) if order else ()), workspace=room, stream=stream)
     torch.cuda.synchronize()
     ref = oa.route(f64(l), k, normalize, scale)
     assert np.array_equal(experts.cpu().numpy(), ref[0]), "experts"
