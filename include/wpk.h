@@ -563,8 +563,9 @@ int wpk_ssm_scan_step(const wpk_ssm_desc *d, const void *x, const void *dt, cons
  * A row has `groups` equal groups, each with a mean of its own.  Values of source outside 0 .. x_rows-1 add nothing. */
 typedef struct wpk_rms_norm_desc {
     int32_t rows, width;            /* rows (0 is allowed, 2^30 at most), columns (65536 at most)        */
-    int32_t groups;                 /* width % groups == 0; a group's width % 128 == 0 where q is given and groups > 1 */
-    int32_t parts, x_rows;          /* rows of x that make one (1 .. 64); rows that x has                */
+    int32_t groups;                 /* width % groups == 0; a group's width % 128 == 0 where q is given and groups > 1; rows * groups
+                                     * below 2^31                                                        */
+    int32_t parts, x_rows;          /* rows of x that make one (1 .. 64); rows that x has, one at least where there are rows to make */
     int32_t dtype;                  /* of x, residual, gain, h and y: WPK_F32, WPK_BF16 or WPK_F16       */
     float eps;                      /* >= 0                                                              */
     int64_t x_stride, residual_stride, h_stride, y_stride, q_stride;   /* >= width, below 2^30; q's % 16 == 0 */
@@ -616,7 +617,7 @@ int wpk_linear_q8_fwd(const wpk_linear_q8_desc *d, const void *x, const float *x
 typedef struct wpk_grouped_linear_desc {
     int32_t groups;                 /* experts, 1 .. 4096                                                */
     int32_t rows;                   /* of y, all experts together (0 is allowed, 2^30 at most)           */
-    int32_t n, k;                   /* columns of y, reduction                                           */
+    int32_t n, k;                   /* columns of y (2^29 at most), reduction                            */
     int32_t x_rows;                 /* rows that x has; >= rows without source                           */
     int32_t dtype;                  /* of x and w                                                        */
     int32_t y_dtype;                /* dtype or WPK_F32; with WPK_E4M3: WPK_F32, WPK_BF16 or WPK_F16     */
@@ -628,7 +629,8 @@ typedef struct wpk_grouped_linear_desc {
     int64_t w_scale_group_stride;   /* 8 bits: between experts' scales, >= their rows * w_scale_stride, below 2^40 */
 } wpk_grouped_linear_desc;
 
-/* Bytes of workspace that wpk_grouped_linear_fwd needs for this descriptor (0: none), or a negative status.  Host only. */
+/* Bytes of workspace that wpk_grouped_linear_fwd needs for this descriptor (0: none, as today for all), or a negative status.  Host
+ * only. */
 int64_t wpk_grouped_linear_workspace_bytes(const wpk_grouped_linear_desc *d);
 
 /* starts: groups + 1 ascending int32 on the device, values outside 0 .. rows clamped to it, NULL with one expert, which then has

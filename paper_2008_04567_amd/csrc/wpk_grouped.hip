@@ -40,6 +40,7 @@ template <typename T, int B, bool GATED> static int launch_grouped_tiles(const L
 //     64 x 2048 x 1536          mean 4: 82 / 75               64 x 2048 x 1024           mean 4: 58 / 55
 //     16 x 4096 x 4096          mean 1: 59 / 76               4: 90 / 100
 //     7 x 300 x 520             mean 95: 6.5 / 6.9 / 10
+//   (mean <= 4 with k >= 2048 stands on the means of 1 and 4; where between 4 and 64 the two cross at such sizes was not measured)
 //   (128 with four steps in LDS, for workgroups that have a compute unit to themselves: 8 x 2048 x 2048, mean 128, 26 against 37)
 //   fp32, rows kernel / tiles of 64 / 128
 //     8 x 2048 x 2048           mean 1: 28 / 74 / 115          32: 77 / 77 / 118         64: 116 / 79 / 119

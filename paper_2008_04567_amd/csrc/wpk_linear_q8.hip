@@ -84,12 +84,15 @@ typedef const __attribute__((address_space(4))) float *Constants;     // read by
 // eight rows' for eight steps, the next eight steps' again and again until these begin, so that the same number of loads is always
 // under way.  (Every other eight rows have the two halves of the eight steps exchanged, so that 16 rows' scales of a step take 16
 // banks.)
+// In the form of 64 rows this is not so: a wave has two loads of scales there, and the compiler keeps the choice between their offsets in
+// scratch memory (12 bytes a lane) and waits for every load under way when it reads it, once a step.  Its steps therefore last as
+// long as their loads do, and its times below are of that.
 // 16384 x 4096 x 4096, bf16: 255 us, 274 to 285 with a residual, 1.93 PFLOP/s and more (a library product with one scale for all
 // takes 192 and no residual).  A step of 256 x 256 takes 1.7 us on a full device where its products alone take 1.04 (the matrix pipes are
 // busy 44 % of the cycles), 1.3 on one workgroup alone.  Without its loads it takes 1.4, without the multiplications by scales 1.4,
-// and fewer cycles came with lower clocks (2.28 to 2.12 GHz): what is left is bound by power more than by any unit.  52 us of the
-// whole, 73 with a residual, are beginnings and ends of tiles (from times at reductions of 128 and more), where all compute units
-// write at once.  Tried without gain: one meeting a step, four steps in LDS (one workgroup a compute unit instead of three: 24 against
+// and fewer cycles came with lower clocks (2.28 to 2.12 GHz): the steps are bound by power more than by any unit.  52 us of the
+// whole, 73 with a residual, are beginnings and ends of tiles (from times at reductions of 128 and more): a compute unit has room for
+// one workgroup, so it is idle while a tile's first steps arrive, and all of them write at once.  Tried without gain: one meeting a step, four steps in LDS (one workgroup a compute unit instead of three: 24 against
 // 13.5 us for 65 x 8512 x 2048), waves of 64 x 64 in tiles of 128, tiles of 128 x 256, a tile's residual asked for a block ahead.
 template <typename T, int BM, int BN, int WM, int WN, int STAGES, bool GROUPED, bool GATED>
 __global__ void __launch_bounds__(64 * WM * WN, (BM + BN) * 128 * STAGES > 73728 ? WM * WN / 4 : WM * WN / 2) linear_q8_kernel(Q8Args q)
@@ -301,7 +304,8 @@ __global__ void __launch_bounds__(64 * WM * WN, (BM + BN) * 128 * STAGES > 73728
 // As product_rows: a workgroup of eight waves owns `width` columns of y (of each half, GATED), 16 NT at most together, and all of
 // up to 16 MT rows.  A wave takes every eighth block of 128 entries of its slice, U of them under way, w straight into registers.  32
 // rows by 8512 columns of 2048: 7.6 us (workgroups of 16 columns 12.8, of 32 11.8, of 36 7.6), of which a launch and one latency are
-// most: w's bytes alone take 3.4.
+// most: w's bytes alone take 3.4.  That is with w in the caches; with weights that rotate through 430 MB 8.7, one row 6.4 instead of 5.0.
+// (By expert x and w are read by flat instructions, and a wait for one block is a wait for all under way: see `uniform`.)
 template <typename T, int MT, int NT, int U, bool GROUPED, bool GATED>
 __global__ void __launch_bounds__(64 * kRowsWaves) linear_q8_rows_kernel(Q8Args q)
 {
@@ -463,8 +467,8 @@ static Q8Shape q8_shape(int64_t m, int64_t n, int64_t k, int dtype)
         slices = kComputeUnits / ((n + s.width - 1) / s.width);
         if (slices > steps / (2 * kRowsWaves)) slices = steps / (2 * kRowsWaves);
     } else {
-        // Small tiles are bound by the chain of meetings and reads in a step, 0.6 us whatever their size, and three workgroups that
-        // share a compute unit hide each other's; large ones by power and read less.  us, tiles of 64 / 128 / 256, bf16 y:
+        // A step of small tiles takes 0.6 us and waits for all loads that are under way (above); three workgroups that share a compute
+        // unit hide part of each other's waits; large ones are bound by power and read less.  us, tiles of 64 / 128 / 256, bf16 y:
         //   m x n x k   1024 x 4096 x 4096   2048 x 8512 x 2048   2048 x 4096 x 4096   4096 x 4096 x 1024   16384 x 4096 x 1024
         //               34 / 40 / 48         64 / 63 / 73         63 / 55 / 62         34 / 40 / 36         125 / 109 / 95
         // Sums in bf16 operands (fp32 y) take more registers and time: 2048 x 4096 x 4096 85 / 98.
@@ -474,6 +478,7 @@ static Q8Shape q8_shape(int64_t m, int64_t n, int64_t k, int dtype)
                  : wide && small > 3 * kComputeUnits && k >= 4096                           ? kQ8Tile128
                                                                                             : kQ8Tile64;
         if (s.form == kQ8Tile64) {
+            // (Of tiles that wait for their loads in every step, as all figures here.)
             // The reduction is cut where steps are worth more than another kernel and the partial sums, written and read: 0.6 us a
             // step in turns of all the workgroups that there is room for, 4 us, and 8 bytes a sum at 4 TB/s.  Cut by 1 / 2 / 4:
             // 128 x 4096 x 4096 22.4 / 17.7 / 15.3 us, 256 x 8512 x 2048 16.5 / 22.0 / 27.7.

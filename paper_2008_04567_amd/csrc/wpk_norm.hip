@@ -29,7 +29,7 @@ __device__ inline int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x +
 // result, so every input is read once; parts of a row are asked for four at a time.  16384 x 4096 bf16 with residual, into h and 8
 // bits: 87 us, 5.4 TB/s (a copy reaches 5.1); eight parts for each of 4096 rows of 2048: 32 us, 5.8 TB/s; 16 rows of 2048: 3.0 us,
 // of which a launch is most.
-// Rows beyond 32768 (P = 8) keep 40 to 140 registers in scratch memory.
+// Rows beyond 32768 (P = 8) keep 40 to 50 registers in scratch memory, 16-bit ones of exactly 65536 columns 126.
 template <typename T, int LANES, int P, bool ALL, bool FAR> __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) rms_norm_kernel(NormArgs a)
 {
     const int kWaves = LANES / 64;

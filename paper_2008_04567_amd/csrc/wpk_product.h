@@ -130,7 +130,9 @@ __device__ inline void group_rows(const LinearArgs &a, int g, int *first, int *l
     }
 }
 
-// an address that all lanes have, where the compiler can see it
+// an address that all lanes have, where the compiler can see it.  (It does not see that this is global memory: by expert x, w and y are
+// read and written by flat instructions, which arrive in any order and count with LDS, so that a wait for one of them is a wait
+// for all that are under way.  Loads that write LDS go by descriptors and are not concerned.)
 template <typename P> __device__ inline P *uniform(P *p)
 {
     const uint64_t v = (uint64_t)p;
@@ -245,7 +247,7 @@ template <typename T, int MT, int NT, int U, bool GROUPED, bool GATED> __device_
     };
     const int step = 64 * kRowsWaves;
     int k = k_begin;
-    // U runs in flight: run u is asked for again as soon as it has been multiplied
+    // U runs in flight: run u is asked for again as soon as it has been multiplied.  (By expert each wait is for all of them: `uniform`.)
     if (k + (U - 1) * step + 64 <= k_end) {
 #pragma unroll
         for (int u = 0; u < U; ++u) fetch(u, k + u * step);

@@ -8,7 +8,8 @@
 namespace wpk {
 
 // A pass over more bytes than this goes past the caches, which would hold none of it for the next call; of fewer, the next call finds
-// its inputs there.  16384 x 4096 bf16 to 8 bits 38 -> 35 us, its norm 95 -> 88; the combination of 4096 x 8 rows of 2048 39 -> 32.
+// its inputs there.  16384 x 4096 bf16 to 8 bits 38 -> 35 us, its norm 95 -> 88; the combination of 4096 x 8 rows of 2048 39 -> 32.  (Each
+// measured one call behind the other; what the product that reads such outputs next gains or loses was not.)
 static const int64_t kFarBytes = 64 << 20;
 
 static const int kScaleBlock = 128;
